@@ -329,6 +329,41 @@ hswa_status hswa_decode_multi(hswa_layer layer, const hswa_shape *shape, const h
                               int32_t max_context_len, void *workspace, size_t workspace_bytes, void *out,
                               void *stream);
 
+/* Eviction by accumulated attention weight, for FULL layers whose cache is held
+ * to a budget (an SWA layer evicts by its window: "KVCache Dual-Pool Design").
+ * Sequence b, of L_b = context_lens[b] cached tokens, keeps
+ * K_b = min(budgets[b], L_b, kept_stride) keys per KV head, each head its own:
+ * the last min(num_recent, K_b), then the first num_sinks as far as there is
+ * room, and of the rest those of the highest scores[b][g][position] (ties: the
+ * lowest position; a NaN counts as -infinity). The kept keys move, in their
+ * order, to positions 0 .. K_b - 1 of `dst`, whose block table row b names the
+ * pages that take them; their values are copied as they are (positions are
+ * encoded in the keys already). The sequence then goes on with `dst`'s row and
+ * a context of K_b: its next token is appended at position K_b, and its old
+ * pages are free for other use once the call's work has completed. Pages of
+ * `src` are only read, so a prefix that other sequences share stays theirs.
+ * `dst` may have the pools of `src`, but not its table, and no page that the
+ * call writes may be one that it reads (the rows of `dst` name pages of their
+ * own; what would be read from a page written to is undefined, no access leaves
+ * the pools).
+ * scores: device fp32 [ns][Hkv][score_stride >= max_context_len] (hswa_decode_scored
+ * builds them). context_lens, budgets: device int32 [ns] (lengths are clamped to
+ * [0, max_context_len], budgets to [0, kept_stride]). kept_out: device int32
+ * [ns][Hkv][kept_stride], receives the kept positions in increasing order;
+ * scores_out: device fp32 [ns][Hkv][scores_out_stride >= kept_stride] or NULL,
+ * receives their scores; it must not overlap `scores`. Entries from K_b on, and
+ * slots of `dst` from K_b on, are left as they were. new_lens_out: device int32
+ * [ns], receives K_b. A kept position whose page id is not in the pool is
+ * stored as a zero key and value, a slot whose page id is not is not stored.
+ * HSWA_ERR_UNSUPPORTED: an SWA layer, or ns * Hkv of 2^22 and more.
+ * HSWA_ERR_CAPACITY: a stride or a table too short for max_context_len or
+ * kept_stride. */
+hswa_status hswa_kv_evict(hswa_layer layer, const hswa_shape *shape, const hswa_cache *src, const hswa_cache *dst,
+                          const float *scores, int32_t score_stride, const int32_t *context_lens,
+                          const int32_t *budgets, int32_t ns, int32_t max_context_len, int32_t num_recent,
+                          int32_t num_sinks, int32_t *kept_out, int32_t kept_stride, float *scores_out,
+                          int32_t scores_out_stride, int32_t *new_lens_out, void *stream);
+
 /* Static string naming a status. */
 const char *hswa_status_string(hswa_status status);
 

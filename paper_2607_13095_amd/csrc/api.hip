@@ -32,6 +32,9 @@ int log2_exact(int32_t x) {
 }
 
 constexpr int32_t kMaxKvHeads = 4096;
+// (sequence, KV head) pairs of a call with a workgroup of up to 1024 threads for each: a grid
+// holds less than 2^32 threads
+constexpr int32_t kMaxGridRows = (1 << 22) - 1;
 
 // Shape checks shared by every device call.
 hswa_status check_shape(const hswa_shape *sh) {
@@ -367,6 +370,45 @@ hswa_status hswa_decode_noalloc(hswa_layer layer, const hswa_shape *shape, const
                                 const int32_t *context_lens, int32_t ns, int32_t max_context_len, void *out,
                                 void *stream) {
   return decode_impl(layer, shape, cache, q, context_lens, ns, 1, max_context_len, nullptr, 0, true, out, stream);
+}
+
+hswa_status hswa_kv_evict(hswa_layer layer, const hswa_shape *shape, const hswa_cache *src, const hswa_cache *dst,
+                          const float *scores, int32_t score_stride, const int32_t *context_lens,
+                          const int32_t *budgets, int32_t ns, int32_t max_context_len, int32_t num_recent,
+                          int32_t num_sinks, int32_t *kept_out, int32_t kept_stride, float *scores_out,
+                          int32_t scores_out_stride, int32_t *new_lens_out, void *stream) {
+  hswa_status st;
+  if ((st = check_layer(layer)) != HSWA_OK) return st;
+  if ((st = check_shape(shape)) != HSWA_OK) return st;
+  if (layer.kind != HSWA_LAYER_FULL) return HSWA_ERR_UNSUPPORTED;
+  if (ns < 0 || max_context_len < 1 || num_recent < 0 || num_sinks < 0 || kept_stride < 1) return HSWA_ERR_INVALID_ARG;
+  if (ns > kMaxGridRows / shape->num_kv_heads) return HSWA_ERR_UNSUPPORTED;
+  hswa::EvictParams p{};
+  if ((st = make_pool(layer, shape, src, p.src)) != HSWA_OK) return st;
+  if ((st = make_pool(layer, shape, dst, p.dst)) != HSWA_OK) return st;
+  const int64_t pg = shape->page_size;
+  if (src->table_stride * pg < max_context_len || dst->table_stride * pg < kept_stride) return HSWA_ERR_CAPACITY;
+  if (score_stride < max_context_len || (scores_out && scores_out_stride < kept_stride)) return HSWA_ERR_CAPACITY;
+  if (src->block_table == dst->block_table) return HSWA_ERR_INVALID_ARG;
+  if (ns == 0) return HSWA_OK;
+  if (!scores || !context_lens || !budgets || !kept_out || !new_lens_out || scores_out == scores)
+    return HSWA_ERR_INVALID_ARG;
+  p.scores = scores;
+  p.ctx_lens = context_lens;
+  p.budgets = budgets;
+  p.kept = kept_out;
+  p.scores_out = scores_out;
+  p.new_lens = new_lens_out;
+  p.score_stride = score_stride;
+  p.out_stride = scores_out_stride;
+  p.ns = ns;
+  p.hkv = shape->num_kv_heads;
+  p.max_ctx = max_context_len;
+  p.max_keep = kept_stride;
+  p.num_recent = num_recent;
+  p.num_sinks = num_sinks;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return finish_launch(hswa::launch_kv_evict(p, s), s);
 }
 
 const char *hswa_status_string(hswa_status status) {

@@ -89,7 +89,21 @@ struct PrefillParams {
   PrefillDesc *ws_desc;   // [spans]
 };
 
+// Eviction (kv_evict.hip): keys of `src` kept by score move to the pages of `dst`.
+struct EvictParams {
+  PoolView src, dst;
+  const float *scores;      // [ns][Hkv][score_stride]
+  const int32_t *ctx_lens;  // [ns]
+  const int32_t *budgets;   // [ns] keys to keep
+  int32_t *kept;            // [ns][Hkv][max_keep] kept positions, in order
+  float *scores_out;        // [ns][Hkv][out_stride] scores of the kept keys, or null
+  int32_t *new_lens;        // [ns]
+  int64_t score_stride, out_stride;
+  int32_t ns, hkv, max_ctx, max_keep, num_recent, num_sinks;
+};
+
 hipError_t launch_kv_append(const AppendParams &p, hipStream_t stream);
+hipError_t launch_kv_evict(const EvictParams &p, hipStream_t stream);
 hipError_t launch_decode(const DecodeParams &p, hipStream_t stream);
 // Decode step with its append in the same launch (decode_append.hip): one
 // query per sequence, whole-range items of at most 8 chunks.

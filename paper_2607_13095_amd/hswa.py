@@ -35,7 +35,8 @@ EXPORTS = ["hswa_ring_pages", "hswa_page_bytes", "hswa_build_block_table", "hswa
            "hswa_prefix_tree_create", "hswa_prefix_tree_destroy", "hswa_prefix_tree_insert",
            "hswa_prefix_tree_match", "hswa_prefix_tree_release_swa", "hswa_prefix_tree_evict",
            "hswa_prefix_tree_stats", "hswa_decode_multi_workspace_bytes", "hswa_decode_multi",
-           "hswa_decode_noalloc", "hswa_decode_append", "hswa_prefill_workspace_bytes", "hswa_prefill_ws"]
+           "hswa_decode_noalloc", "hswa_decode_append", "hswa_prefill_workspace_bytes", "hswa_prefill_ws",
+           "hswa_kv_evict"]
 
 # bytes of the library's fixed device array behind hswa_decode_noalloc
 NOALLOC_SCRATCH_BYTES = 128 << 20
@@ -101,6 +102,7 @@ def load():
         "hswa_decode_multi": (ctypes.c_int, [LP, SP, CP, P, P, I32, I32, I32, P, SZ, P, P]),
         "hswa_decode_noalloc": (ctypes.c_int, [LP, SP, CP, P, P, I32, I32, P, P]),
         "hswa_decode_append": (ctypes.c_int, [LP, SP, CP, P, P, P, P, I32, I32, P, SZ, P, P]),
+        "hswa_kv_evict": (ctypes.c_int, [LP, SP, CP, CP, P, I32, P, P, I32, I32, I32, I32, P, I32, P, I32, P, P]),
         "hswa_allocator_create": (ctypes.c_int, [ctypes.POINTER(_AllocConfig), ctypes.POINTER(P)]),
         "hswa_allocator_destroy": (None, [P]),
         "hswa_allocator_admit": (ctypes.c_int, [P, I32, I64, I32]),
@@ -199,15 +201,16 @@ def _ptr(t, name, dtypes, numel=0):
 
 
 _TORCH = None
-_BF16 = _I32 = _WS = ()  # accepted dtypes
+_BF16 = _I32 = _F32 = _WS = ()  # accepted dtypes
 
 
 def _torch():
-    global _TORCH, _BF16, _I32, _WS
+    global _TORCH, _BF16, _I32, _F32, _WS
     if _TORCH is None:
         import torch
 
-        _BF16, _I32, _WS = (torch.bfloat16,), (torch.int32,), (torch.uint8, torch.float32, torch.int32)
+        _BF16, _I32, _F32 = (torch.bfloat16,), (torch.int32,), (torch.float32,)
+        _WS = (torch.uint8, torch.float32, torch.int32)
         _TORCH = torch
     return _TORCH
 
@@ -507,6 +510,42 @@ def decode_noalloc(layer: Layer, shape: Shape, cache: Cache, q, context_lens, ma
     st = load().hswa_decode_noalloc(layer.c(), shape.ref(), cache.ref(), qp, cp, ns, int(max_context_len),
                                     o, _stream(stream))
     _check(st, "hswa_decode_noalloc")
+
+
+def _check_device(cache: Cache, *tensors):
+    """The tensors of a call live on one GPU, the current one (its stream runs the call)."""
+    dev = _torch().cuda.current_device()
+    for t in (cache.k_pool, cache.v_pool, cache.block_table, *tensors):
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"a tensor on GPU {t.get_device()}, the current one is {dev}")
+
+
+def kv_evict(layer: Layer, shape: Shape, src: Cache, dst: Cache, scores, context_lens, budgets, max_context_len: int,
+             kept_out, new_lens_out, num_recent: int = 0, num_sinks: int = 0, scores_out=None, stream=None):
+    """Keep each KV head's highest-scored keys (and the first num_sinks, the last
+    num_recent) and move them from the pages of `src` to those of `dst`; scores
+    [NS, Hkv, >= max_context_len], scores_out [NS, Hkv, >= K] fp32, kept_out
+    [NS, Hkv, K] int32 with K the most keys that a sequence keeps; see
+    hswa_kv_evict."""
+    _torch()
+    ns, hkv = context_lens.numel(), shape.num_kv_heads
+    for t, name in ((scores, "scores"), (kept_out, "kept_out"), (scores_out, "scores_out")):
+        if t is None and name != "scores_out":
+            raise TypeError(f"{name} must be a torch tensor")
+        if t is not None and (t.dim() != 3 or tuple(t.shape[:2]) != (ns, hkv)):
+            raise ValueError(f"{name} must be [NS, Hkv, positions] = [{ns}, {hkv}, ...]")
+    sp, kp = _ptr(scores, "scores", _F32), _ptr(kept_out, "kept_out", _I32)
+    so = _ptr(scores_out, "scores_out", _F32)
+    cp, bp = _ptr(context_lens, "context_lens", _I32, ns), _ptr(budgets, "budgets", _I32, ns)
+    np_ = _ptr(new_lens_out, "new_lens_out", _I32, ns)
+    _check_cache(shape, src, ns)
+    _check_cache(shape, dst, ns)
+    _check_device(src, dst.k_pool, dst.v_pool, dst.block_table, scores, kept_out, scores_out, context_lens, budgets,
+                  new_lens_out)
+    st = load().hswa_kv_evict(layer.c(), shape.ref(), src.ref(), dst.ref(), sp, int(scores.shape[2]), cp, bp, ns,
+                              int(max_context_len), int(num_recent), int(num_sinks), kp, int(kept_out.shape[2]), so,
+                              int(scores_out.shape[2]) if scores_out is not None else 0, np_, _stream(stream))
+    _check(st, "hswa_kv_evict")
 
 
 # ---------------------------------------------------------------------------
