@@ -329,6 +329,31 @@ hswa_status hswa_decode_multi(hswa_layer layer, const hswa_shape *shape, const h
                               int32_t max_context_len, void *workspace, size_t workspace_bytes, void *out,
                               void *stream);
 
+/* hswa_decode_multi (num_queries = 1: hswa_decode) of a FULL layer that also
+ * adds every key's attention weight to a running score, what hswa_kv_evict goes
+ * by: for every sequence b, KV head g and position j < c_b,
+ *     scores_out[b][g][j] = scores_in[b][g][j]
+ *         + sum over the call's queries that see j and the Hq / Hkv query heads
+ *           of g of softmax_j(scale * <q, k_j>).
+ * Entries from position c_b on are left as they were. A step adds its own
+ * token's weight too; the last tokens of a prompt, given as the num_queries
+ * queries of one call, score the whole prompt (its keys appended first).
+ * scores_in: device fp32 [ns][Hkv][score_stride], or NULL for zeros; may be
+ * scores_out (in place), must not overlap it otherwise. scores_out: the same
+ * shape; score_stride >= max_context_len. Weights and sums are fp32, added in an
+ * order that depends on nothing but the call's shape and the lengths. A key on
+ * a page id outside the pool is left out, as in hswa_decode, and adds nothing.
+ * The other arguments and the output rows are as in hswa_decode_multi (rows may
+ * differ from its in the last bit: their sums are not of rounded probabilities);
+ * workspace >= hswa_decode_scored_workspace_bytes, for contexts of any length.
+ * SWA layers return HSWA_ERR_UNSUPPORTED: they evict by their window. */
+size_t hswa_decode_scored_workspace_bytes(const hswa_shape *shape, int32_t ns, int32_t num_queries,
+                                          int32_t max_context_len);
+hswa_status hswa_decode_scored(hswa_layer layer, const hswa_shape *shape, const hswa_cache *cache, const void *q,
+                               const int32_t *context_lens, int32_t ns, int32_t num_queries, int32_t max_context_len,
+                               const float *scores_in, float *scores_out, int32_t score_stride, void *workspace,
+                               size_t workspace_bytes, void *out, void *stream);
+
 /* Eviction by accumulated attention weight, for FULL layers whose cache is held
  * to a budget (an SWA layer evicts by its window: "KVCache Dual-Pool Design").
  * Sequence b, of L_b = context_lens[b] cached tokens, keeps

@@ -111,11 +111,12 @@ hswa_status check_multi_window(hswa_layer layer, const hswa_shape *sh, int32_t n
   return HSWA_OK;
 }
 
-DecodeGeometry decode_geometry(const hswa_shape *sh, int32_t ns, int32_t max_ctx, int32_t nq) {
+// `always`: split whatever the length (for calls that keep every row's log-sum-exp).
+DecodeGeometry decode_geometry(const hswa_shape *sh, int32_t ns, int32_t max_ctx, int32_t nq, bool always = false) {
   DecodeGeometry g{};
   const int group = sh->num_q_heads / sh->num_kv_heads;
   g.split_len = hswa::decode_split_len(ns, sh->num_kv_heads, group, max_ctx);
-  if (max_ctx <= g.split_len) {  // single pass, no workspace
+  if (max_ctx <= g.split_len && !always) {  // single pass, no workspace
     g.max_splits = 1;
     return g;
   }
@@ -126,6 +127,34 @@ DecodeGeometry decode_geometry(const hswa_shape *sh, int32_t ns, int32_t max_ctx
   g.o_bytes = align_up(rows * sh->head_dim * sizeof(float), 256);
   g.total_bytes = g.o_bytes + align_up(rows * sizeof(float), 256);
   return g;
+}
+
+// Scored decode: the split partials, then the rows' log-sum-exps.
+struct ScoredGeometry {
+  DecodeGeometry d;
+  size_t total_bytes;
+};
+
+ScoredGeometry scored_geometry(const hswa_shape *sh, int32_t ns, int32_t max_ctx, int32_t nq) {
+  ScoredGeometry g{};
+  g.d = decode_geometry(sh, ns, max_ctx, nq, true);
+  g.total_bytes = g.d.total_bytes + align_up((size_t)ns * nq * sh->num_q_heads * sizeof(float), 256);
+  return g;
+}
+
+// What every decode call tells its kernels besides the pool and the split.
+void decode_params(hswa::DecodeParams &p, const hswa_shape *shape, const void *q, const int32_t *context_lens,
+                   int32_t ns, int32_t num_queries, int32_t max_context_len, void *out) {
+  p.q = static_cast<const uint16_t *>(q);
+  p.ctx_lens = context_lens;
+  p.out = static_cast<uint16_t *>(out);
+  p.ns = ns;
+  p.hq = shape->num_q_heads;
+  p.hkv = shape->num_kv_heads;
+  p.group = p.hq / p.hkv;
+  p.max_ctx = max_context_len;
+  p.nq = num_queries;
+  p.scale_log2 = shape->scale * 1.4426950408889634f;
 }
 
 }  // namespace
@@ -286,16 +315,7 @@ hswa_status decode_impl(hswa_layer layer, const hswa_shape *shape, const hswa_ca
   if (append && (!k_new || !v_new)) return HSWA_ERR_INVALID_ARG;
   hswa::DecodeParams p{};
   p.pool = pv;
-  p.q = static_cast<const uint16_t *>(q);
-  p.ctx_lens = context_lens;
-  p.out = static_cast<uint16_t *>(out);
-  p.ns = ns;
-  p.hq = shape->num_q_heads;
-  p.hkv = shape->num_kv_heads;
-  p.group = p.hq / p.hkv;
-  p.max_ctx = max_context_len;
-  p.nq = num_queries;
-  p.scale_log2 = shape->scale * 1.4426950408889634f;
+  decode_params(p, shape, q, context_lens, ns, num_queries, max_context_len, out);
   if (layer.kind == HSWA_LAYER_FULL) {
     const DecodeGeometry geo = decode_geometry(shape, ns, max_context_len, num_queries);
     p.split_len = geo.split_len;
@@ -370,6 +390,44 @@ hswa_status hswa_decode_noalloc(hswa_layer layer, const hswa_shape *shape, const
                                 const int32_t *context_lens, int32_t ns, int32_t max_context_len, void *out,
                                 void *stream) {
   return decode_impl(layer, shape, cache, q, context_lens, ns, 1, max_context_len, nullptr, 0, true, out, stream);
+}
+
+size_t hswa_decode_scored_workspace_bytes(const hswa_shape *shape, int32_t ns, int32_t num_queries,
+                                          int32_t max_context_len) {
+  if (check_shape(shape) != HSWA_OK || ns < 1 || max_context_len < 1) return 0;
+  if (num_queries < 1 || num_queries > kMaxQueries) return 0;
+  return scored_geometry(shape, ns, max_context_len, num_queries).total_bytes;
+}
+
+hswa_status hswa_decode_scored(hswa_layer layer, const hswa_shape *shape, const hswa_cache *cache, const void *q,
+                               const int32_t *context_lens, int32_t ns, int32_t num_queries, int32_t max_context_len,
+                               const float *scores_in, float *scores_out, int32_t score_stride, void *workspace,
+                               size_t workspace_bytes, void *out, void *stream) {
+  hswa_status st;
+  if ((st = check_layer(layer)) != HSWA_OK) return st;
+  if ((st = check_shape(shape)) != HSWA_OK) return st;
+  if (layer.kind != HSWA_LAYER_FULL) return HSWA_ERR_UNSUPPORTED;
+  if (ns < 0 || max_context_len < 1 || num_queries < 1 || num_queries > kMaxQueries) return HSWA_ERR_INVALID_ARG;
+  hswa::ScoredParams p{};
+  if ((st = make_pool(layer, shape, cache, p.d.pool)) != HSWA_OK) return st;
+  if ((int64_t)cache->table_stride * shape->page_size < (int64_t)max_context_len) return HSWA_ERR_CAPACITY;
+  if (score_stride < max_context_len) return HSWA_ERR_CAPACITY;
+  if (ns == 0) return HSWA_OK;
+  if (!q || !context_lens || !out || !scores_out || !workspace) return HSWA_ERR_INVALID_ARG;
+  const ScoredGeometry geo = scored_geometry(shape, ns, max_context_len, num_queries);
+  if (workspace_bytes < geo.total_bytes) return HSWA_ERR_CAPACITY;
+  decode_params(p.d, shape, q, context_lens, ns, num_queries, max_context_len, out);
+  p.d.split_len = geo.d.split_len;
+  p.d.max_splits = geo.d.max_splits;
+  char *ws = static_cast<char *>(workspace);
+  p.d.ws_o = reinterpret_cast<float *>(ws);
+  p.d.ws_lse = reinterpret_cast<float *>(ws + geo.d.o_bytes);
+  p.d.row_lse = reinterpret_cast<float *>(ws + geo.d.total_bytes);
+  p.scores_in = scores_in;
+  p.scores_out = scores_out;
+  p.stride = score_stride;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return finish_launch(hswa::launch_decode_scored(p, s), s);
 }
 
 hswa_status hswa_kv_evict(hswa_layer layer, const hswa_shape *shape, const hswa_cache *src, const hswa_cache *dst,

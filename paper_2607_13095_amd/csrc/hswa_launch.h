@@ -64,6 +64,9 @@ struct DecodeParams {
   // FULL split decode of one new token per sequence: the kernel also
   // stores the token (k_new / v_new) in its slot and takes its key from them
   int32_t split_append;
+  float *row_lse;             // scored decode: [ns * nq * Hq], the rows' log2 sum-exps
+  const int32_t *start;       // suffix decode: [ns], first key (a multiple of 32) of each sequence
+  const int64_t *suffix_per;  // and the chunks of a span
 };
 
 // Split prefill: the query tile at the start of a span, for the merge.
@@ -102,7 +105,16 @@ struct EvictParams {
   int32_t ns, hkv, max_ctx, max_keep, num_recent, num_sinks;
 };
 
+// Decode that also adds every key's attention weight to a score (decode_scored.hip).
+struct ScoredParams {
+  DecodeParams d;          // split (max_splits > 1), with row_lse
+  const float *scores_in;  // [ns][Hkv][stride], or null for zeros; may be scores_out
+  float *scores_out;
+  int64_t stride;
+};
+
 hipError_t launch_kv_append(const AppendParams &p, hipStream_t stream);
+hipError_t launch_decode_scored(const ScoredParams &p, hipStream_t stream);
 hipError_t launch_kv_evict(const EvictParams &p, hipStream_t stream);
 hipError_t launch_decode(const DecodeParams &p, hipStream_t stream);
 // Decode step with its append in the same launch (decode_append.hip): one

@@ -36,7 +36,7 @@ EXPORTS = ["hswa_ring_pages", "hswa_page_bytes", "hswa_build_block_table", "hswa
            "hswa_prefix_tree_match", "hswa_prefix_tree_release_swa", "hswa_prefix_tree_evict",
            "hswa_prefix_tree_stats", "hswa_decode_multi_workspace_bytes", "hswa_decode_multi",
            "hswa_decode_noalloc", "hswa_decode_append", "hswa_prefill_workspace_bytes", "hswa_prefill_ws",
-           "hswa_kv_evict"]
+           "hswa_kv_evict", "hswa_decode_scored_workspace_bytes", "hswa_decode_scored"]
 
 # bytes of the library's fixed device array behind hswa_decode_noalloc
 NOALLOC_SCRATCH_BYTES = 128 << 20
@@ -102,6 +102,8 @@ def load():
         "hswa_decode_multi": (ctypes.c_int, [LP, SP, CP, P, P, I32, I32, I32, P, SZ, P, P]),
         "hswa_decode_noalloc": (ctypes.c_int, [LP, SP, CP, P, P, I32, I32, P, P]),
         "hswa_decode_append": (ctypes.c_int, [LP, SP, CP, P, P, P, P, I32, I32, P, SZ, P, P]),
+        "hswa_decode_scored_workspace_bytes": (SZ, [SP, I32, I32, I32]),
+        "hswa_decode_scored": (ctypes.c_int, [LP, SP, CP, P, P, I32, I32, I32, P, P, I32, P, SZ, P, P]),
         "hswa_kv_evict": (ctypes.c_int, [LP, SP, CP, CP, P, I32, P, P, I32, I32, I32, I32, P, I32, P, I32, P, P]),
         "hswa_allocator_create": (ctypes.c_int, [ctypes.POINTER(_AllocConfig), ctypes.POINTER(P)]),
         "hswa_allocator_destroy": (None, [P]),
@@ -518,6 +520,50 @@ def _check_device(cache: Cache, *tensors):
     for t in (cache.k_pool, cache.v_pool, cache.block_table, *tensors):
         if t is not None and t.get_device() != dev:
             raise ValueError(f"a tensor on GPU {t.get_device()}, the current one is {dev}")
+
+
+def _queries(q, context_lens):
+    """(sequences, queries of each) of q [NS, nq, Hq, D], or [NS, Hq, D] for one query each."""
+    if q.dim() not in (3, 4):
+        raise ValueError("q must be [NS, num_queries, Hq, D] or [NS, Hq, D]")
+    if context_lens.numel() != int(q.shape[0]):
+        raise ValueError("one context length per sequence")
+    return int(q.shape[0]), int(q.shape[1]) if q.dim() == 4 else 1
+
+
+def _workspace(workspace):
+    if workspace is None:
+        return None, 0
+    return _ptr(workspace, "workspace", _WS), workspace.numel() * workspace.element_size()
+
+
+def decode_scored_workspace_bytes(shape: Shape, ns: int, num_queries: int, max_context_len: int) -> int:
+    return int(load().hswa_decode_scored_workspace_bytes(shape.ref(), int(ns), int(num_queries), int(max_context_len)))
+
+
+def decode_scored(layer: Layer, shape: Shape, cache: Cache, q, context_lens, max_context_len: int, scores_in,
+                  scores_out, out, workspace=None, stream=None):
+    """Decode of q [NS, nq, Hq, D] (or [NS, Hq, D]) that adds every key's
+    attention weight to its score: scores_out = scores_in + weights
+    [NS, Hkv, >= max_context_len] fp32; scores_in may be scores_out, or None for
+    zeros; see hswa_decode_scored."""
+    _torch()
+    ns, nq = _queries(q, context_lens)
+    for t, name in ((scores_out, "scores_out"), (scores_in, "scores_in")):
+        if t is None and name == "scores_out":
+            raise TypeError("scores_out must be a torch tensor")
+        if t is not None and (t.dim() != 3 or tuple(t.shape) != (ns, shape.num_kv_heads, int(scores_out.shape[-1]))):
+            raise ValueError(f"{name} must be [NS, Hkv, positions] = [{ns}, {shape.num_kv_heads}, ...], both alike")
+    row = nq * shape.num_q_heads * shape.head_dim
+    qp, cp = _ptr(q, "q", _BF16, ns * row), _ptr(context_lens, "context_lens", _I32, ns)
+    o = _ptr(out, "out", _BF16, ns * row)
+    si, so = _ptr(scores_in, "scores_in", _F32), _ptr(scores_out, "scores_out", _F32)
+    wp, wbytes = _workspace(workspace)
+    _check_cache(shape, cache, ns)
+    _check_device(cache, q, context_lens, scores_in, scores_out, out, workspace)
+    st = load().hswa_decode_scored(layer.c(), shape.ref(), cache.ref(), qp, cp, ns, nq, int(max_context_len), si, so,
+                                   int(scores_out.shape[2]), wp, wbytes, o, _stream(stream))
+    _check(st, "hswa_decode_scored")
 
 
 def kv_evict(layer: Layer, shape: Shape, src: Cache, dst: Cache, scores, context_lens, budgets, max_context_len: int,

@@ -76,3 +76,43 @@ def test_kv_evict_binding_refusals():
         call(kept_out=None)
     with pytest.raises(ValueError):  # not on the GPU
         call()
+
+
+def _scored(layer=None, shape=None, cache=None, q=FAKE, ctx=FAKE, ns=2, nq=1, maxc=500, si=None, so=FAKE, stride=500,
+            ws=FAKE, wsb=1 << 40, out=FAKE):
+    return hswa.load().hswa_decode_scored(layer or _full(), ctypes.byref(shape or _shape()),
+                                          ctypes.byref(cache or _cache()), q, ctx, ns, nq, maxc, si, so, stride, ws, wsb,
+                                          out, None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(ns=0), OK),
+    (dict(layer=hswa._Layer(hswa.HSWA_LAYER_SWA, 128)), UNSUPPORTED),
+    (dict(layer=hswa._Layer(hswa.HSWA_LAYER_SWA_PAGED, 128)), UNSUPPORTED),
+    (dict(shape=_shape(d=64)), UNSUPPORTED), (dict(shape=_shape(scale=0.0)), INVALID),
+    (dict(ns=-1), INVALID), (dict(nq=0), INVALID), (dict(nq=65), INVALID), (dict(maxc=0), INVALID),
+    (dict(stride=499), CAPACITY), (dict(cache=_cache(7)), CAPACITY), (dict(wsb=1000), CAPACITY),
+    (dict(q=None), INVALID), (dict(ctx=None), INVALID), (dict(so=None), INVALID), (dict(out=None), INVALID),
+    (dict(ws=None), INVALID),
+])
+def test_decode_scored_refusals(kw, code):
+    assert _scored(**kw) == code
+
+
+def test_decode_scored_workspace():
+    sh = hswa.Shape(64, 8)
+    assert hswa.decode_scored_workspace_bytes(sh, 2, 1, 100) > 0
+    assert hswa.decode_scored_workspace_bytes(sh, 2, 1, 5000) > hswa.decode_workspace_bytes(sh, 2, 5000)
+    for a in ((0, 1, 100), (2, 0, 100), (2, 65, 100), (2, 1, 0)):
+        assert hswa.decode_scored_workspace_bytes(sh, *a) == 0
+
+
+def test_decode_scored_binding_refusals():
+    shape, cache, layer = hswa.Shape(4, 2, 128, 16), _cpu_cache(), hswa.Layer.full()
+    q, ctx = torch.zeros((2, 4, 128), dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32)
+    s = torch.zeros((2, 2, 32))
+    for bad, kind in ((dict(q=q[0]), ValueError), (dict(q=q[:1]), ValueError), (dict(s=s[:1]), ValueError),
+                      (dict(s=None), TypeError), (dict(si=torch.zeros((2, 2, 31))), ValueError), (dict(), ValueError)):
+        a = dict(q=q, s=s, si=None, **{}) | bad
+        with pytest.raises(kind):
+            hswa.decode_scored(layer, shape, cache, a["q"], ctx, 32, a["si"], a["s"], q)
