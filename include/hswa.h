@@ -329,6 +329,36 @@ hswa_status hswa_decode_multi(hswa_layer layer, const hswa_shape *shape, const h
                               int32_t max_context_len, void *workspace, size_t workspace_bytes, void *out,
                               void *stream);
 
+/* hswa_decode_multi (num_queries = 1: hswa_decode) for batches in which runs of
+ * consecutive sequences share a prefix ("SWA-Aware Prefix Cache Tree": equal
+ * token prefixes share their cached slots; n samples of one prompt, many users
+ * of one system prompt): a FULL layer reads the keys of a prefix once for the
+ * whole run. Group i is the sequences cu_groups[i] .. cu_groups[i + 1] - 1; their
+ * first shared_lens[i] positions hold the same keys and values, so that reading
+ * them through any one row of the block table gives the same (rows that name
+ * the same pages, or copies). Of the shared positions the call uses as such the
+ * whole multiples of 64 that every query of the group's sequences sees (at most
+ * the shortest context - num_queries + 1; a sequence without a context does not
+ * count), read through the row of the group's first sequence with a context;
+ * the rest, and sequences of no group, are read as hswa_decode_multi reads them.
+ * Every row of the table is complete all the same: which entries are read is no
+ * part of the contract. The outputs are hswa_decode_multi's up to rounding.
+ * cu_groups: device int32 [num_groups + 1], non-decreasing, within [0, ns];
+ * shared_lens: device int32 [num_groups] (values above max_shared_len are
+ * clamped to it, values below 64 share nothing); num_groups <= ns;
+ * max_shared_len: host. Offsets out of range are clamped and decreasing ones make
+ * empty groups. workspace >= hswa_decode_shared_workspace_bytes (FULL only: an
+ * SWA layer reads its window, the call is hswa_decode_multi's; so it is where
+ * no prefix can be shared: no group, one sequence, max_shared_len below 64).
+ * The other arguments are as in hswa_decode_multi. */
+size_t hswa_decode_shared_workspace_bytes(const hswa_shape *shape, int32_t ns, int32_t num_queries,
+                                          int32_t max_context_len, int32_t num_groups, int32_t max_shared_len);
+hswa_status hswa_decode_shared(hswa_layer layer, const hswa_shape *shape, const hswa_cache *cache, const void *q,
+                               const int32_t *context_lens, int32_t ns, int32_t num_queries, int32_t max_context_len,
+                               const int32_t *cu_groups, const int32_t *shared_lens, int32_t num_groups,
+                               int32_t max_shared_len, void *workspace, size_t workspace_bytes, void *out,
+                               void *stream);
+
 /* hswa_decode_multi (num_queries = 1: hswa_decode) of a FULL layer that also
  * adds every key's attention weight to a running score, what hswa_kv_evict goes
  * by: for every sequence b, KV head g and position j < c_b,

@@ -22,7 +22,7 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libhswa.so")
 SOURCES = ["api.hip", "kv_append.hip", "decode.hip", "prefill.hip", "prefill_window.hip", "prefill_run.hip",
            "noalloc.hip", "decode_append.hip",
-           "decode_scored.hip", "kv_evict.hip"]
+           "decode_scored.hip", "decode_shared.hip", "kv_evict.hip"]
 HOST_SOURCES = ["allocator.cpp", "prefix_tree.cpp"]
 CXX = os.environ.get("CXX", shutil.which("g++") or "g++")
 CXXFLAGS = ["-O2", "-std=c++17", "-fPIC", "-Wall", "-I", os.path.join(ROOT, "include")]

@@ -142,6 +142,47 @@ ScoredGeometry scored_geometry(const hswa_shape *sh, int32_t ns, int32_t max_ctx
   return g;
 }
 
+// Shared-prefix decode: the plan, the partials of the own keys, those of the
+// prefixes.
+struct SharedGeometry {
+  DecodeGeometry d;
+  size_t groups, group_units, group_rows, own_units, start, group_of, own, ws_o, ws_lse, total_bytes;
+};
+
+SharedGeometry shared_geometry(const hswa_shape *sh, int32_t ns, int32_t max_ctx, int32_t nq, int32_t ng) {
+  SharedGeometry g{};
+  g.d = decode_geometry(sh, ns, max_ctx, nq, true);
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t o = at;
+    at += align_up(bytes, 256);
+    return o;
+  };
+  take(sizeof(hswa::SharedHead));
+  g.groups = take((size_t)ng * sizeof(hswa::SharedGroup));
+  g.group_units = take(((size_t)ng + 1) * sizeof(int64_t));
+  g.group_rows = take((size_t)ng * sizeof(int64_t));
+  g.own_units = take((size_t)ns * sizeof(int64_t));
+  g.start = take((size_t)ns * sizeof(int32_t));
+  g.group_of = take((size_t)ns * sizeof(int32_t));
+  g.own = take(g.d.total_bytes);
+  // a piece of a prefix has the rows of its columns, in 16s for a group's; each span adds at most a
+  // workgroup's columns; a group that shares has two sequences or more
+  const size_t cols = (size_t)ns * nq * (sh->num_q_heads / sh->num_kv_heads);
+  const size_t sharing = (size_t)(ng < ns / 2 ? ng : ns / 2);
+  const size_t rows = sh->num_kv_heads * (cols + 15 * sharing) + (size_t)hswa::kSharedSpans * hswa::kSharedCols;
+  g.ws_o = take(rows * sh->head_dim * sizeof(float));
+  g.ws_lse = take(rows * sizeof(float));
+  g.total_bytes = at;
+  return g;
+}
+
+// Whether a call may have prefixes worth reading once: two sequences of a
+// group and a tile of shared keys.
+bool shared_fits(int32_t ns, int32_t num_groups, int32_t max_shared_len) {
+  return ns >= 2 && num_groups >= 1 && max_shared_len >= hswa::kSharedTile;
+}
+
 // What every decode call tells its kernels besides the pool and the split.
 void decode_params(hswa::DecodeParams &p, const hswa_shape *shape, const void *q, const int32_t *context_lens,
                    int32_t ns, int32_t num_queries, int32_t max_context_len, void *out) {
@@ -390,6 +431,61 @@ hswa_status hswa_decode_noalloc(hswa_layer layer, const hswa_shape *shape, const
                                 const int32_t *context_lens, int32_t ns, int32_t max_context_len, void *out,
                                 void *stream) {
   return decode_impl(layer, shape, cache, q, context_lens, ns, 1, max_context_len, nullptr, 0, true, out, stream);
+}
+
+size_t hswa_decode_shared_workspace_bytes(const hswa_shape *shape, int32_t ns, int32_t num_queries,
+                                          int32_t max_context_len, int32_t num_groups, int32_t max_shared_len) {
+  if (check_shape(shape) != HSWA_OK || ns < 1 || max_context_len < 1 || num_groups < 0 || num_groups > ns) return 0;
+  if (num_queries < 1 || num_queries > kMaxQueries || max_shared_len < 0) return 0;
+  if (!shared_fits(ns, num_groups, max_shared_len))
+    return hswa_decode_multi_workspace_bytes(shape, ns, num_queries, max_context_len);
+  return shared_geometry(shape, ns, max_context_len, num_queries, num_groups).total_bytes;
+}
+
+hswa_status hswa_decode_shared(hswa_layer layer, const hswa_shape *shape, const hswa_cache *cache, const void *q,
+                               const int32_t *context_lens, int32_t ns, int32_t num_queries, int32_t max_context_len,
+                               const int32_t *cu_groups, const int32_t *shared_lens, int32_t num_groups,
+                               int32_t max_shared_len, void *workspace, size_t workspace_bytes, void *out,
+                               void *stream) {
+  if (num_groups < 0 || max_shared_len < 0 || (ns >= 0 && num_groups > ns)) return HSWA_ERR_INVALID_ARG;
+  if (num_groups > 0 && (!cu_groups || !shared_lens)) return HSWA_ERR_INVALID_ARG;
+  if (layer.kind != HSWA_LAYER_FULL || !shared_fits(ns, num_groups, max_shared_len))
+    return hswa_decode_multi(layer, shape, cache, q, context_lens, ns, num_queries, max_context_len, workspace,
+                             workspace_bytes, out, stream);
+  hswa_status st;
+  if ((st = check_shape(shape)) != HSWA_OK) return st;
+  if (max_context_len < 1 || num_queries < 1 || num_queries > kMaxQueries) return HSWA_ERR_INVALID_ARG;
+  hswa::SharedParams p{};
+  if ((st = make_pool(layer, shape, cache, p.d.pool)) != HSWA_OK) return st;
+  if ((int64_t)cache->table_stride * shape->page_size < (int64_t)max_context_len) return HSWA_ERR_CAPACITY;
+  if (!q || !context_lens || !out || !workspace) return HSWA_ERR_INVALID_ARG;
+  // (column and row numbers of the plan are 32-bit)
+  if ((int64_t)ns * num_queries * shape->num_q_heads > INT32_MAX) return HSWA_ERR_UNSUPPORTED;
+  const SharedGeometry geo = shared_geometry(shape, ns, max_context_len, num_queries, num_groups);
+  if (workspace_bytes < geo.total_bytes) return HSWA_ERR_CAPACITY;
+  decode_params(p.d, shape, q, context_lens, ns, num_queries, max_context_len, out);
+  p.d.split_len = geo.d.split_len;
+  p.d.max_splits = geo.d.max_splits;
+  char *ws = static_cast<char *>(workspace);
+  p.d.ws_o = reinterpret_cast<float *>(ws + geo.own);
+  p.d.ws_lse = reinterpret_cast<float *>(ws + geo.own + geo.d.o_bytes);
+  p.cu_groups = cu_groups;
+  p.shared_lens = shared_lens;
+  p.ng = num_groups;
+  p.max_shared = max_shared_len;
+  p.head = reinterpret_cast<hswa::SharedHead *>(ws);
+  p.groups = reinterpret_cast<hswa::SharedGroup *>(ws + geo.groups);
+  p.group_units = reinterpret_cast<int64_t *>(ws + geo.group_units);
+  p.group_rows = reinterpret_cast<int64_t *>(ws + geo.group_rows);
+  p.own_units = reinterpret_cast<int64_t *>(ws + geo.own_units);
+  p.start = reinterpret_cast<int32_t *>(ws + geo.start);
+  p.group_of = reinterpret_cast<int32_t *>(ws + geo.group_of);
+  p.ws_o = reinterpret_cast<float *>(ws + geo.ws_o);
+  p.ws_lse = reinterpret_cast<float *>(ws + geo.ws_lse);
+  p.d.start = p.start;
+  p.d.suffix_per = &p.head->own_per;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return finish_launch(hswa::launch_decode_shared(p, s), s);
 }
 
 size_t hswa_decode_scored_workspace_bytes(const hswa_shape *shape, int32_t ns, int32_t num_queries,

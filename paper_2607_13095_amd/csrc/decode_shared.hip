@@ -1,0 +1,626 @@
+// Decode for batches in which runs of consecutive sequences share a prefix
+// ("SWA-Aware Prefix Cache Tree": equal token prefixes share their cached
+// slots): the prefix's keys are read once for all sequences of a run instead of
+// once for each.
+//
+// Attention over a split key range is merged by the log-sum-exp identity, so a
+// row is the merge of its part over the prefix and its part over the
+// sequence's own keys. Four kernels:
+//   plan    one workgroup: the keys a group shares (whole tiles of 64 that every
+//           one of its queries sees), prefix sums of the work
+//   own     the keys from there on, one sequence at a time: the split decode
+//           (decode_kernels.h), bound by reading them
+//   prefix  all queries of a group against the shared keys, tiles of 64 keys
+//           in LDS under up to 256 columns, a column being a (sequence,
+//           query, head) of one KV head: bound by the matrix products and the
+//           exponentials when the group is large, by reading the keys when
+//           it is small
+//   merge   the partials of each row
+// The prefix kernel cuts the key tiles of all (group, KV head, 256 columns), in
+// that order, into equal spans, one per workgroup, each on a compute unit. Its
+// two phases (matrix products, softmax with the staging of tiles) alternate
+// between two groups of four waves, one wave of each on a SIMD, as in prefill.hip.
+// Every shared tile is whole and seen by every query, so it needs no masks.
+#include <algorithm>
+#include <type_traits>
+
+#include "decode_kernels.h"
+
+namespace hswa {
+namespace {
+
+constexpr int kPlanThreads = 1024;
+constexpr int kPlanWaves = kPlanThreads / kWave;
+constexpr int kGroupLanes = 16;     // lanes that look over a group's sequences
+constexpr int kThreads = 512;
+constexpr int kKT = kSharedTile;    // keys per tile
+constexpr int kBufs = 4;            // LDS tile buffers: two being read, one stored, one loading
+constexpr int kTileCols = kSharedCols;  // columns of a workgroup
+constexpr int kKTileBytes = kKT * kHeadDim * 2;
+constexpr int kBufBytes = 2 * kKTileBytes;
+constexpr int kStage = kKT * kHeadDim / 8 / kThreads;  // 16-byte pieces per thread per tile (K or V)
+static_assert(kStage == 2, "piece i of a thread belongs to 32-key block i");
+constexpr int kAhead = 4;           // LDS operand reads in flight ahead of the matrix products
+constexpr float kLaneSumLimit = 4096.f;  // a lane's share of a row sum above which the running maximum is raised
+constexpr int kMinSpan = 4;         // least key tiles of a span
+constexpr int kMinOwn = 4;          // least chunks of a span of the own keys
+constexpr int kXcds = 8;
+
+__device__ __forceinline__ int64_t max64(int64_t a, int64_t b) { return a > b ? a : b; }
+
+// Inclusive scan over the workgroup of the plan with `op`; `last`: the result of all.
+template <typename Op>
+__device__ __forceinline__ int64_t block_scan(int64_t x, int64_t (&part)[kPlanWaves], int64_t &last, Op op) {
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+#pragma unroll
+  for (int off = 1; off < kWave; off <<= 1) {
+    const int64_t t = __shfl_up(x, off, kWave);
+    if (lane >= off) x = op(x, t);
+  }
+  __syncthreads();  // (part was read by the scan before)
+  if (lane == kWave - 1) part[wave] = x;
+  __syncthreads();
+  last = part[0];
+  for (int w = 1; w < kPlanWaves; ++w) {
+    if (w == wave) x = op(x, last);
+    last = op(last, part[w]);
+  }
+  return x;
+}
+
+__global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(SharedParams p) {
+  __shared__ int64_t part[kPlanWaves];
+  __shared__ int32_t cut[kPlanThreads + 1];  // first sequences of the groups at hand, made non-decreasing
+  const auto add = [](int64_t a, int64_t b) { return a + b; };
+  const auto most = [](int64_t a, int64_t b) { return max64(a, b); };
+  const DecodeParams &d = p.d;
+  const int tid = threadIdx.x;
+  for (int b = tid; b < d.ns; b += kPlanThreads) {
+    p.start[b] = 0;
+    p.group_of[b] = -1;
+  }
+  int64_t units = 0, rows = 0;  // before the groups at hand
+  int carry = 0;
+  for (int i0 = 0; i0 < p.ng; i0 += kPlanThreads) {
+    const int n = min(kPlanThreads, p.ng - i0);
+    // offsets that are out of range or decrease make empty groups, never overlapping ones
+    auto offset = [&](int i) { return (int64_t)min(max(p.cu_groups[i0 + i], 0), d.ns); };
+    int64_t all;
+    const int64_t c = block_scan(max64(tid < n ? offset(tid) : 0, carry), part, all, most);
+    if (tid < n) cut[tid] = (int)c;
+    if (tid == 0) cut[n] = (int)max64(all, offset(n));
+    __syncthreads();
+    carry = cut[n];
+    const int gl = tid & (kGroupLanes - 1);
+    for (int i = tid / kGroupLanes; i < n; i += kPlanThreads / kGroupLanes) {
+      const int first = cut[i], end = cut[i + 1];
+      // its sequences with a context: the shortest context, their number, the first of them
+      int least = d.max_ctx, count = 0, leader = end;
+      for (int b = first + gl; b < end; b += kGroupLanes) {
+        const int ctx = d.ctx_lens[b];
+        if (ctx >= 1) {
+          least = min(least, ctx);
+          leader = min(leader, b);
+          ++count;
+        }
+      }
+#pragma unroll
+      for (int off = 1; off < kGroupLanes; off <<= 1) {
+        least = min(least, __shfl_xor(least, off, kGroupLanes));
+        leader = min(leader, __shfl_xor(leader, off, kGroupLanes));
+        count += __shfl_xor(count, off, kGroupLanes);
+      }
+      // the first query of each sequence sees the keys up to its own position
+      const int shared = min(min(p.shared_lens[i0 + i], p.max_shared), least - d.nq + 1);
+      const int tiles = count >= 2 && shared > 0 ? shared / kKT : 0;
+      if (gl == 0) {
+        SharedGroup g;
+        g.first = first;
+        g.leader = leader;
+        g.tiles = tiles;
+        g.cols = tiles > 0 ? (end - first) * d.nq * d.group : 0;
+        p.groups[i0 + i] = g;
+      }
+      if (tiles > 0)
+        for (int b = first + gl; b < end; b += kGroupLanes) {
+          p.start[b] = d.ctx_lens[b] >= 1 ? tiles * kKT : 0;
+          p.group_of[b] = i0 + i;
+        }
+    }
+    __syncthreads();
+    int64_t gu = 0, gr = 0;
+    if (tid < n) {
+      const SharedGroup &g = p.groups[i0 + tid];
+      gu = (int64_t)d.hkv * ((g.cols + kTileCols - 1) / kTileCols) * g.tiles;
+      gr = (int64_t)d.hkv * ((g.cols + kCols - 1) / kCols * kCols);
+    }
+    int64_t tu, tr;
+    const int64_t su = block_scan(gu, part, tu, add), sr = block_scan(gr, part, tr, add);
+    if (tid < n) {
+      p.group_units[i0 + tid] = units + su - gu;
+      p.group_rows[i0 + tid] = rows + sr - gr;
+    }
+    units += tu;
+    rows += tr;
+  }
+  // the own keys, in chunks
+  __syncthreads();
+  const int H = d.hkv * ((d.nq * d.group + d.item_cols - 1) / d.item_cols);
+  int64_t chunks = 0, longest = 0;
+  for (int b0 = 0; b0 < d.ns; b0 += kPlanThreads) {
+    const int64_t n = seq_chunks<kSuffix>(d, b0 + tid);
+    int64_t total, m;
+    const int64_t s = block_scan(n, part, total, add);
+    block_scan(n, part, m, most);
+    if (b0 + tid < d.ns) p.own_units[b0 + tid] = (chunks + s - n) * H;
+    chunks += total;
+    longest = max64(longest, m);
+  }
+  if (tid == 0) {
+    p.group_units[p.ng] = units;
+    p.head->units = units;
+    p.head->per = max64(kMinSpan, (units + kSharedSpans - 1) / kSharedSpans);
+    // spans of the own keys: at most max_splits pieces of a sequence's
+    const int64_t even = (chunks * H + d.span_waves - 1) / d.span_waves;
+    p.head->own_per = max64(max64(kMinOwn, even), (longest + d.max_splits - 2) / (d.max_splits - 1));
+  }
+}
+
+struct __attribute__((aligned(16))) TileBufs {
+  unsigned char b[kBufs * kBufBytes];
+};
+
+// Key tiles [j0, j1) of a group (its leader's row of the block table) for KV
+// head g and the columns from col0 on: partial rows to slot, slot + 1, ... of
+// the workspace. kCG: 16-column groups of a wave. kPage: keys of a page, 64
+// standing for 64 and more.
+template <int kCG, int kPage>
+__device__ __forceinline__ void prefix_tiles(const SharedParams &p, TileBufs &bufs, const SharedGroup &grp, int g,
+                                             int col0, int j0, int j1, int64_t slot) {
+  unsigned char *const s_lds = bufs.b;
+  const DecodeParams &d = p.d;
+  const PoolView &pv = d.pool;
+  const int tid = threadIdx.x, lane = tid & (kWave - 1);
+  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int r = lane & 15, q = lane >> 4;
+  const int shift = pv.pg_shift;
+  const float c2 = d.scale_log2;
+  const int ncols = min(grp.cols - col0, kTileCols);
+  // column group cg of the wave: columns 16 (8 cg + wave) .. + 15
+  const bool active = 16 * wave < ncols;  // (the first one; a wave without columns only stages)
+
+  u32x4 qf[kCG][4];
+#pragma unroll
+  for (int cg = 0; cg < kCG; ++cg) {
+    const int col = 16 * (8 * cg + wave) + r;
+    const bool valid = col < ncols;
+    const int x = col0 + (valid ? col : 0), per = d.nq * d.group;
+    const int m = x / per, rem = x - m * per, qi = rem / d.group, hh = rem - qi * d.group;
+    const uint16_t *qrow =
+        d.q + (((int64_t)(grp.first + m) * d.nq + qi) * d.hq + (int64_t)g * d.group + hh) * kHeadDim;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const u32x4 v = ldg128(qrow + 32 * t + 8 * q);
+      const u32x4 z = {0u, 0u, 0u, 0u};
+      qf[cg][t] = valid ? v : z;
+    }
+  }
+
+  // ---- staging: global -> registers -> LDS, in MFMA operand order ----
+  // K: the pool's 32-key blocks as they are; V^T: block (h, dt) holds, for lane
+  // r + 16 q, keys 32 h + 8 q .. + 7 of dim 16 dt + r.
+  constexpr int kPages = kKT / kPage;
+  const int vq = (tid >> 4) & 3, vdim = 16 * (tid >> 6) + (tid & 15);
+  const int last_lp = (kKT * j1 - 1) >> shift;
+  int tab_lp0 = (kKT * j0) >> shift;
+  auto load_tab = [&](int lp0) {  // lane i: the entry of logical page lp0 + i
+    const int lp = lp0 + lane;
+    return lp <= last_lp ? pv.table[(int64_t)grp.leader * pv.stride + lp] : -1;
+  };
+  int tab_page = load_tab(tab_lp0), tab_next = load_tab(tab_lp0 + kWave);
+  uint32_t held = 0;  // bit 4 (j % 8) + n: the n-th 16 keys of tile j are in the pool
+  u32x4 sk[kStage], sv[kStage];
+  auto fetch = [&](int j, u32x4 (&k)[kStage], u32x4 (&v)[kStage]) __attribute__((always_inline)) {
+    const int kt = kKT * j, lp = kt >> shift;
+    if (lp - tab_lp0 >= kWave) {
+      tab_lp0 += kWave;
+      tab_page = tab_next;
+      tab_next = load_tab(tab_lp0 + kWave);
+    }
+    int page[kPages];
+    uint32_t bits = 0;
+#pragma unroll
+    for (int n = 0; n < kPages; ++n) {
+      const int e = __builtin_amdgcn_readlane(tab_page, lp + n - tab_lp0);
+      page[n] = e >= 0 && e < pv.num_pages ? e : -1;
+      bits |= page[n] >= 0 ? ((1u << (4 / kPages)) - 1u) << (n * (4 / kPages)) : 0u;
+    }
+    const int at = 4 * (j & 7);
+    held = (held & ~(15u << at)) | (bits << at);
+    auto page_off = [&](int pg) {  // byte offset of the page-head (of the tile in it)
+      const uint64_t o = ((uint64_t)((uint32_t)max(pg, 0)) * (uint32_t)d.hkv + (uint32_t)g) << (shift + kHeadDimShift + 1);
+      return kPage == 64 ? o + ((uint64_t)((uint32_t)kt & ((1u << shift) - 1u)) << (kHeadDimShift + 1)) : o;
+    };
+#pragma unroll
+    for (int i = 0; i < kStage; ++i) {
+      uint64_t ko, vo;
+      uint32_t kl, vl;
+      if constexpr (kPage == 16) {
+        const uint64_t o0 = page_off(page[2 * i]), o1 = page_off(page[2 * i + 1]);
+        ko = tid & 8 ? o1 : o0;  // of this lane's K rows and V keys
+        vo = vq & 2 ? o1 : o0;
+        kl = (uint32_t)((tid >> 4) * 128 + (tid & 7) * 16);
+        vl = (uint32_t)(vdim * 32 + (vq & 1) * 16);
+      } else {
+        ko = vo = page_off(page[kPage == 32 ? i : 0]) + (kPage == 32 ? 0 : 8192 * i);
+        kl = (uint32_t)tid * 16u;
+        vl = (uint32_t)(vdim * 32 + vq * 8) * 2u;
+      }
+      k[i] = ldg128_global(reinterpret_cast<const char *>(pv.k_pool) + ko + kl);
+      v[i] = ldg128_global(reinterpret_cast<const char *>(pv.v_pool) + vo + vl);
+    }
+    if (bits != 15u) {  // a page outside the pool: its keys are left out, their values zero
+#pragma unroll
+      for (int i = 0; i < kStage; ++i) {
+        const u32x4 z = {0u, 0u, 0u, 0u};
+        v[i] = (bits >> (2 * i + (vq >> 1))) & 1u ? v[i] : z;
+      }
+    }
+  };
+  auto buf_off = [&](int buf) { return (uint32_t)__builtin_amdgcn_readfirstlane(buf * kBufBytes); };
+  auto lds128 = [&](uint32_t off) { return reinterpret_cast<u32x4 *>(s_lds + off); };
+  auto store_tile = [&](int buf, const u32x4 (&k)[kStage], const u32x4 (&v)[kStage]) __attribute__((always_inline)) {
+    const uint32_t a = buf_off(buf) + tid * 16;
+#pragma unroll
+    for (int i = 0; i < kStage; ++i) {
+      *lds128(a + i * (kKTileBytes / 2)) = k[i];
+      *lds128(a + kKTileBytes + i * (kKTileBytes / 2)) = v[i];
+    }
+  };
+
+  float m[kCG], lsum[kCG];
+  f32x4 acc[kCG][8];
+#pragma unroll
+  for (int cg = 0; cg < kCG; ++cg) {
+    m[cg] = -FLT_MAX;
+    lsum[cg] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) acc[cg][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const uint32_t op_lane = lane * 16;
+  auto qk_half = [&](int buf, int h, f32x4 (&sc)[2][kCG]) {
+    const uint32_t a = buf_off(buf) + op_lane + h * (kKTileBytes / 2);
+#pragma unroll
+    for (int cg = 0; cg < kCG; ++cg) sc[0][cg] = sc[1][cg] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const u32x4 ka = *lds128(a + 1024 * t);
+      const u32x4 kb = *lds128(a + 4096 + 1024 * t);
+#pragma unroll
+      for (int cg = 0; cg < kCG; ++cg) {
+        sc[0][cg] = mfma16x16x32(ka, qf[cg][t], sc[0][cg]);
+        sc[1][cg] = mfma16x16x32(kb, qf[cg][t], sc[1][cg]);
+      }
+    }
+  };
+  auto pv_tile = [&](int buf, const u32x4 (&pf)[2][kCG]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t a = buf_off(buf) + kKTileBytes + op_lane + h * (kKTileBytes / 2);
+      u32x4 vf[8];
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) vf[dt] = *lds128(a + 1024 * dt);
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt)
+#pragma unroll
+        for (int cg = 0; cg < kCG; ++cg) acc[cg][dt] = mfma16x16x32(vf[dt], pf[h][cg], acc[cg][dt]);
+    }
+  };
+  // Exponentials against the running maximum as it stands; it is raised, and the
+  // tile's exponentials taken again, only if some lane's share of a row sum
+  // exceeds 2^12 (an infinite one counts): numerator and denominator share the
+  // maximum, so the result is the same. It starts at -FLT_MAX, so that a masked
+  // score gives 0 and the first finite one raises it.
+  auto tile_exp = [&](const f32x4 (&sc)[2][2][kCG], u32x4 (&pf)[2][kCG], float (&ts)[kCG]) {
+#pragma unroll
+    for (int cg = 0; cg < kCG; ++cg) {
+      const float mc = m[cg];
+      ts[cg] = 0.f;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float pr[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) pr[e] = fast_exp2(fmaf(sc[h][e >> 2][cg][e & 3], c2, -mc));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) pf[h][cg][j] = pack_bf16x2(pr[2 * j], pr[2 * j + 1]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) ts[cg] = dot2_bf16_ones(pf[h][cg][j], ts[cg]);
+      }
+    }
+  };
+  auto softmax_tile = [&](int j, f32x4 (&sc)[2][2][kCG], u32x4 (&pf)[2][kCG]) {
+    const uint32_t bits = (held >> (4 * (j & 7))) & 15u;
+    if (bits != 15u) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const bool in = (bits >> (2 * h + (q >> 1))) & 1u;
+#pragma unroll
+        for (int cg = 0; cg < kCG; ++cg)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) sc[h][e >> 2][cg][e & 3] = in ? sc[h][e >> 2][cg][e & 3] : -INFINITY;
+      }
+    }
+    float ts[kCG];
+    tile_exp(sc, pf, ts);
+    bool raise = false;
+#pragma unroll
+    for (int cg = 0; cg < kCG; ++cg) raise = raise || !(ts[cg] <= kLaneSumLimit);
+    if (__builtin_amdgcn_ballot_w64(raise) != 0) {
+#pragma unroll
+      for (int cg = 0; cg < kCG; ++cg) {
+        float s8[2][8];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) s8[h][e] = sc[h][e >> 2][cg][e & 3];
+        const float cmax = max_xor32(max_xor16(max2(max8(s8[0]), max8(s8[1])))) * c2;
+        const bool up = cmax > m[cg];
+        const float alpha = up ? fast_exp2(m[cg] - cmax) : 1.f;
+        m[cg] = up ? cmax : m[cg];
+        lsum[cg] *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) acc[cg][dt] *= alpha;
+      }
+      tile_exp(sc, pf, ts);
+    }
+#pragma unroll
+    for (int cg = 0; cg < kCG; ++cg) lsum[cg] += ts[cg];
+  };
+
+  const int ntiles = j1 - j0;
+  {
+    u32x4 k0[kStage], v0[kStage], k1[kStage], v1[kStage];
+    fetch(j0, k0, v0);
+    if (ntiles > 1) fetch(j0 + 1, k1, v1);
+    if (ntiles > 2) fetch(j0 + 2, sk, sv);
+    store_tile(0, k0, v0);
+    if (ntiles > 1) store_tile(1, k1, v1);
+  }
+  __syncthreads();
+  f32x4 sc[2][2][kCG];
+  u32x4 pf[2][kCG];
+  // matrix phase of tile jt (from j0 on): PV of tile jt - 1, QK^T of tile jt,
+  // at raised issue priority, operand reads kAhead reads ahead of the products
+  auto matrix_phase = [&](int jt, auto first_tag) __attribute__((always_inline)) {
+    constexpr bool kFirst = decltype(first_tag)::value;
+    constexpr int kReads = kFirst ? 16 : 32;
+    if (!active) return;
+    const int buf = jt & (kBufs - 1);
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(2);
+    if constexpr (!kFirst) pv_tile((jt + kBufs - 1) & (kBufs - 1), pf);
+    qk_half(buf, 0, sc[0]);
+    qk_half(buf, 1, sc[1]);
+    __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+    for (int i = 0; i < kReads - kAhead; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, kCG, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, kCG * kAhead, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(0);
+  };
+  auto softmax_phase = [&](int jt) __attribute__((always_inline)) {
+    if (jt + 2 < ntiles) store_tile((jt + 2) & (kBufs - 1), sk, sv);
+    if (jt + 3 < ntiles) fetch(j0 + jt + 3, sk, sv);
+    if (active) softmax_tile(j0 + jt, sc, pf);
+  };
+  auto tile_barrier = [&]() {
+    __builtin_amdgcn_sched_barrier(0);
+    __syncthreads();
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // One barrier per tile. Between barriers t and t + 1 waves 0-3 run the matrix
+  // phase of tile t, then its softmax phase; waves 4-7 first the softmax phase
+  // of tile t - 1, then the matrix phase of tile t. Read in between are tiles t
+  // (K) and t - 1 (V), stored are tiles t + 2 (waves 0-3) and t + 1 (waves 4-7),
+  // whose buffers were last read before barrier t.
+  constexpr std::true_type kFirstTile{};
+  constexpr std::false_type kNextTile{};
+  if (wave < kThreads / kWave / 2) {
+    matrix_phase(0, kFirstTile);
+    softmax_phase(0);
+    tile_barrier();
+    for (int jt = 1; jt < ntiles; ++jt) {
+      matrix_phase(jt, kNextTile);
+      softmax_phase(jt);
+      tile_barrier();
+    }
+  } else {
+    matrix_phase(0, kFirstTile);
+    tile_barrier();
+    for (int jt = 1; jt < ntiles; ++jt) {
+      softmax_phase(jt - 1);
+      matrix_phase(jt, kNextTile);
+      tile_barrier();
+    }
+    softmax_phase(ntiles - 1);
+  }
+  if (!active) return;
+  pv_tile((ntiles + kBufs - 1) & (kBufs - 1), pf);
+#pragma unroll
+  for (int cg = 0; cg < kCG; ++cg) {
+    const float l = sum_xor32(sum_xor16(lsum[cg]));
+    const int col = 16 * (8 * cg + wave) + r;
+    if (col >= ncols) continue;
+    const float inv = l > 0.f ? 1.f / l : 0.f;  // (no key in the pool: o = 0, log-sum-exp -inf)
+    float *dst = p.ws_o + (slot + col) * kHeadDim + 4 * q;
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<f32x4 *>(dst + 16 * dt) = acc[cg][dt] * inv;
+    if (q == 0) p.ws_lse[slot + col] = m[cg] + __log2f(l);
+  }
+}
+
+template <int kPage>
+__global__ __launch_bounds__(kThreads) void shared_prefix_kernel(SharedParams p) {
+  __shared__ TileBufs bufs;
+  // workgroup ids go to the XCDs round-robin: an XCD gets consecutive spans,
+  // which read the same keys for other columns, or neighbouring ones
+  const int span = (int)(blockIdx.x % kXcds) * (kSharedSpans / kXcds) + (int)(blockIdx.x / kXcds);
+  const int64_t per = p.head->per;
+  int64_t u = span * per;
+  const int64_t u1 = u + per < p.head->units ? u + per : p.head->units;
+  if (u >= u1) return;
+  int gi = 0;  // the group holding unit u: the last one that starts at or before it
+  for (int hi = p.ng; hi - gi > 1;) {
+    const int mid = (gi + hi) >> 1;
+    if (p.group_units[mid] <= u) gi = mid;
+    else hi = mid;
+  }
+  for (;;) {
+    while (u >= p.group_units[gi + 1]) ++gi;
+    const SharedGroup grp = p.groups[gi];
+    const int ntc = (grp.cols + kTileCols - 1) / kTileCols;
+    const int64_t rem = u - p.group_units[gi];
+    const int seg = (int)(rem / grp.tiles), j0 = (int)(rem - (int64_t)seg * grp.tiles);
+    const int g = seg / ntc, col0 = (seg - g * ntc) * kTileCols;
+    const int j1 = (int)min((int64_t)grp.tiles, j0 + (u1 - u));
+    const int64_t rows = (grp.cols + kCols - 1) / kCols * kCols;
+    // pieces follow each other by tile or by span: no two share a row
+    const int64_t slot = p.group_rows[gi] + g * rows + col0 + (int64_t)span * kTileCols;
+    if (grp.cols - col0 <= kTileCols / 2) prefix_tiles<1, kPage>(p, bufs, grp, g, col0, j0, j1, slot);
+    else prefix_tiles<2, kPage>(p, bufs, grp, g, col0, j0, j1, slot);
+    u += j1 - j0;
+    if (u >= u1) return;
+    __syncthreads();  // every wave has read the tile buffers
+  }
+}
+
+// Merge of a row's pieces, those of the prefix and then its own: a wave per row,
+// the two half-waves take even and odd pieces, four output dims a lane.
+__global__ __launch_bounds__(kMergeThreads) void shared_merge_kernel(SharedParams p) {
+  const DecodeParams &d = p.d;
+  const int lane = threadIdx.x & (kWave - 1);
+  const int64_t idx = (int64_t)blockIdx.x * (kMergeThreads / kWave) + uni((int)(threadIdx.x / kWave));
+  if (idx >= (int64_t)d.ns * d.nq * d.hq) return;
+  const int b = (int)(idx / ((int64_t)d.nq * d.hq));
+  const int half = lane >> 5, d4 = (lane & 31) * 4;
+  u32x2 *dst = reinterpret_cast<u32x2 *>(d.out + idx * kHeadDim + d4);
+  const u32x2 zero = {0u, 0u};
+  const int ctx = min(d.ctx_lens[b], d.max_ctx);
+  if (ctx < 1) {
+    if (half == 0) *dst = zero;
+    return;
+  }
+  const int rem = (int)(idx - (int64_t)b * d.nq * d.hq);
+  const int qi = rem / d.hq, head = rem - qi * d.hq;
+  const int g = head / d.group, hh = head - g * d.group;
+  // pieces of the prefix: rows first, first + 256, ... of its partials
+  int n0 = 0;
+  int64_t first = 0;
+  const int start = p.start[b];
+  if (start > 0) {
+    const int gi = p.group_of[b];
+    const SharedGroup grp = p.groups[gi];
+    const int col = ((b - grp.first) * d.nq + qi) * d.group + hh;
+    const int ntc = (grp.cols + kTileCols - 1) / kTileCols;
+    const int64_t seg = p.group_units[gi] + (int64_t)(g * ntc + col / kTileCols) * grp.tiles;
+    const int64_t s0 = seg / p.head->per, s1 = (seg + grp.tiles - 1) / p.head->per;
+    n0 = (int)(s1 - s0) + 1;
+    first = p.group_rows[gi] + (int64_t)g * ((grp.cols + kCols - 1) / kCols * kCols) + col + s0 * kTileCols;
+  }
+  // and of its own keys
+  const int nch = (ctx - start + kChunk - 1) / kChunk;
+  int n1 = 0;
+  if (nch > 0) {
+    const int hchunks = (d.nq * d.group + d.item_cols - 1) / d.item_cols;
+    const int64_t seg = p.own_units[b] + (int64_t)(g * hchunks + (qi * d.group + hh) / d.item_cols) * nch;
+    n1 = (int)((seg + nch - 1) / p.head->own_per - seg / p.head->own_per) + 1;
+  }
+  if (n0 == 0 && n1 == 1) return;  // one piece: the decode kernel wrote the row
+  const int n = n0 + n1;
+  auto lse_of = [&](int s) {
+    return s < n0 ? p.ws_lse[first + (int64_t)s * kTileCols] : d.ws_lse[idx * d.max_splits + s - n0];
+  };
+  float mx = -INFINITY;
+  for (int s = lane; s < n; s += kWave) mx = fmaxf(mx, lse_of(s));
+#pragma unroll
+  for (int off = 8; off >= 1; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off, kWave));
+  mx = max_xor32(max_xor16(mx));
+  if (mx == -INFINITY) {  // a row that sees no key
+    if (half == 0) *dst = zero;
+    return;
+  }
+  const float *po0 = p.ws_o + first * kHeadDim + d4, *po1 = d.ws_o + (idx * d.max_splits - n0) * kHeadDim + d4;
+  float wsum = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < n; s0 += kWave) {
+    const int s = s0 + lane;
+    const float w = s < n ? fast_exp2(lse_of(s) - mx) : 0.f;
+    const int m = min(kWave, n - s0);
+    for (int k0 = 0; k0 < m; k0 += 16) {
+      f32x4 v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int pc = k0 + 2 * k + half, sp = s0 + pc;
+        const f32x4 z = {0.f, 0.f, 0.f, 0.f};
+        const float *src = sp < n0 ? po0 + (int64_t)sp * kTileCols * kHeadDim : po1 + (int64_t)sp * kHeadDim;
+        v[k] = pc < m ? *reinterpret_cast<const f32x4 *>(src) : z;
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int pc = k0 + 2 * k + half;
+        const float wk = __shfl(w, min(pc, kWave - 1), kWave);
+        const float wv = pc < m ? wk : 0.f;
+        wsum += wv;
+        o += wv * v[k];
+      }
+    }
+  }
+  wsum = sum_xor32(wsum);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o[i] = sum_xor32(o[i]);
+  const float inv = 1.f / wsum;
+  if (half == 0) {
+    u32x2 w2;
+    w2[0] = pack_bf16x2(o[0] * inv, o[1] * inv);
+    w2[1] = pack_bf16x2(o[2] * inv, o[3] * inv);
+    *dst = w2;
+  }
+}
+
+template <int kCGd>
+hipError_t launch_cg(const SharedParams &p0, hipStream_t stream) {
+  SharedParams p = p0;
+  DecodeParams &d = p.d;
+  d.item_cols = kCols * kCGd;
+  const bool one_page = d.pool.pg_shift >= 5;
+  hipError_t e = one_page ? resident_split_waves<true, kCGd, kSuffix>(d.span_waves)
+                          : resident_split_waves<false, kCGd, kSuffix>(d.span_waves);
+  if (e != hipSuccess) return e;
+  if ((e = launch_kernel(shared_plan_kernel, dim3(1), dim3(kPlanThreads), stream, p)) != hipSuccess) return e;
+  const dim3 grid((unsigned)(d.span_waves / kWaves)), block(kWave * kWaves);
+  e = one_page ? launch_kernel(decode_kernel<true, true, kCGd, kSuffix>, grid, block, stream, d)
+               : launch_kernel(decode_kernel<true, false, kCGd, kSuffix>, grid, block, stream, d);
+  if (e != hipSuccess) return e;
+  const dim3 spans(kSharedSpans), threads(kThreads);
+  switch (d.pool.pg_shift) {
+    case 4: e = launch_kernel(shared_prefix_kernel<16>, spans, threads, stream, p); break;
+    case 5: e = launch_kernel(shared_prefix_kernel<32>, spans, threads, stream, p); break;
+    default: e = launch_kernel(shared_prefix_kernel<64>, spans, threads, stream, p);
+  }
+  if (e != hipSuccess) return e;
+  const int64_t rows = (int64_t)d.ns * d.nq * d.hq;
+  constexpr int per_block = kMergeThreads / kWave;
+  return launch_kernel(shared_merge_kernel, dim3((unsigned)((rows + per_block - 1) / per_block)), dim3(kMergeThreads),
+                       stream, p);
+}
+
+}  // namespace
+
+hipError_t launch_decode_shared(const SharedParams &p, hipStream_t stream) {
+  return p.d.nq * p.d.group > kCols ? launch_cg<2>(p, stream) : launch_cg<1>(p, stream);
+}
+
+}  // namespace hswa

@@ -92,6 +92,37 @@ struct PrefillParams {
   PrefillDesc *ws_desc;   // [spans]
 };
 
+// Decode over shared prefixes (decode_shared.hip). The plan, in the workspace:
+constexpr int kSharedTile = 64;    // keys of a tile of the prefix
+constexpr int kSharedCols = 256;   // (sequence, query, head) columns of a workgroup
+constexpr int kSharedSpans = 256;  // workgroups of the prefix kernel, one per compute unit
+struct SharedGroup {
+  int32_t first;   // its first sequence
+  int32_t leader;  // the first with a context: the prefix is read from its row of the table
+  int32_t tiles;   // key tiles taken as shared (0: none)
+  int32_t cols;    // columns of a KV head (0 without tiles)
+};
+struct SharedHead {
+  int64_t units;    // key tiles of all (group, KV head, kSharedCols columns)
+  int64_t per;      // of them, those of a span
+  int64_t own_per;  // chunks of a span of the own keys
+};
+struct SharedParams {
+  DecodeParams d;              // the own keys; start and suffix_per point into the plan
+  const int32_t *cu_groups;    // [ng + 1]
+  const int32_t *shared_lens;  // [ng]
+  int32_t ng, max_shared;
+  SharedHead *head;
+  SharedGroup *groups;   // [ng]
+  int64_t *group_units;  // [ng + 1] units before each group
+  int64_t *group_rows;   // [ng] rows of partials before each group
+  int64_t *own_units;    // [ns] chunks (of every KV head) before each sequence's
+  int32_t *start;        // [ns] shared keys of each sequence
+  int32_t *group_of;     // [ns]
+  float *ws_o;           // partial rows of the prefixes
+  float *ws_lse;
+};
+
 // Eviction (kv_evict.hip): keys of `src` kept by score move to the pages of `dst`.
 struct EvictParams {
   PoolView src, dst;
@@ -114,6 +145,7 @@ struct ScoredParams {
 };
 
 hipError_t launch_kv_append(const AppendParams &p, hipStream_t stream);
+hipError_t launch_decode_shared(const SharedParams &p, hipStream_t stream);
 hipError_t launch_decode_scored(const ScoredParams &p, hipStream_t stream);
 hipError_t launch_kv_evict(const EvictParams &p, hipStream_t stream);
 hipError_t launch_decode(const DecodeParams &p, hipStream_t stream);

@@ -36,7 +36,8 @@ EXPORTS = ["hswa_ring_pages", "hswa_page_bytes", "hswa_build_block_table", "hswa
            "hswa_prefix_tree_match", "hswa_prefix_tree_release_swa", "hswa_prefix_tree_evict",
            "hswa_prefix_tree_stats", "hswa_decode_multi_workspace_bytes", "hswa_decode_multi",
            "hswa_decode_noalloc", "hswa_decode_append", "hswa_prefill_workspace_bytes", "hswa_prefill_ws",
-           "hswa_kv_evict", "hswa_decode_scored_workspace_bytes", "hswa_decode_scored"]
+           "hswa_decode_shared_workspace_bytes", "hswa_decode_shared", "hswa_kv_evict",
+           "hswa_decode_scored_workspace_bytes", "hswa_decode_scored"]
 
 # bytes of the library's fixed device array behind hswa_decode_noalloc
 NOALLOC_SCRATCH_BYTES = 128 << 20
@@ -102,6 +103,8 @@ def load():
         "hswa_decode_multi": (ctypes.c_int, [LP, SP, CP, P, P, I32, I32, I32, P, SZ, P, P]),
         "hswa_decode_noalloc": (ctypes.c_int, [LP, SP, CP, P, P, I32, I32, P, P]),
         "hswa_decode_append": (ctypes.c_int, [LP, SP, CP, P, P, P, P, I32, I32, P, SZ, P, P]),
+        "hswa_decode_shared_workspace_bytes": (SZ, [SP, I32, I32, I32, I32, I32]),
+        "hswa_decode_shared": (ctypes.c_int, [LP, SP, CP, P, P, I32, I32, I32, P, P, I32, I32, P, SZ, P, P]),
         "hswa_decode_scored_workspace_bytes": (SZ, [SP, I32, I32, I32]),
         "hswa_decode_scored": (ctypes.c_int, [LP, SP, CP, P, P, I32, I32, I32, P, P, I32, P, SZ, P, P]),
         "hswa_kv_evict": (ctypes.c_int, [LP, SP, CP, CP, P, I32, P, P, I32, I32, I32, I32, P, I32, P, I32, P, P]),
@@ -535,6 +538,34 @@ def _workspace(workspace):
     if workspace is None:
         return None, 0
     return _ptr(workspace, "workspace", _WS), workspace.numel() * workspace.element_size()
+
+
+def decode_shared_workspace_bytes(shape: Shape, ns: int, num_queries: int, max_context_len: int, num_groups: int,
+                                  max_shared_len: int) -> int:
+    return int(load().hswa_decode_shared_workspace_bytes(shape.ref(), int(ns), int(num_queries), int(max_context_len),
+                                                         int(num_groups), int(max_shared_len)))
+
+
+def decode_shared(layer: Layer, shape: Shape, cache: Cache, q, context_lens, max_context_len: int, cu_groups,
+                  shared_lens, max_shared_len: int, out, workspace=None, stream=None):
+    """Decode of q [NS, nq, Hq, D] (or [NS, Hq, D]) where the sequences
+    cu_groups[i] .. cu_groups[i + 1] - 1 share their first shared_lens[i]
+    positions, which are read once for all of them; see hswa_decode_shared."""
+    _torch()
+    ns, nq = _queries(q, context_lens)
+    ng = shared_lens.numel()
+    if cu_groups.numel() != ng + 1:
+        raise ValueError("cu_groups has one entry more than shared_lens")
+    row = nq * shape.num_q_heads * shape.head_dim
+    qp, cp = _ptr(q, "q", _BF16, ns * row), _ptr(context_lens, "context_lens", _I32, ns)
+    gp, lp = _ptr(cu_groups, "cu_groups", _I32, ng + 1), _ptr(shared_lens, "shared_lens", _I32, ng)
+    o = _ptr(out, "out", _BF16, ns * row)
+    wp, wbytes = _workspace(workspace)
+    _check_cache(shape, cache, ns)
+    _check_device(cache, q, context_lens, cu_groups, shared_lens, out, workspace)
+    st = load().hswa_decode_shared(layer.c(), shape.ref(), cache.ref(), qp, cp, ns, nq, int(max_context_len), gp, lp,
+                                   ng, int(max_shared_len), wp, wbytes, o, _stream(stream))
+    _check(st, "hswa_decode_shared")
 
 
 def decode_scored_workspace_bytes(shape: Shape, ns: int, num_queries: int, max_context_len: int) -> int:

@@ -116,3 +116,48 @@ def test_decode_scored_binding_refusals():
         a = dict(q=q, s=s, si=None, **{}) | bad
         with pytest.raises(kind):
             hswa.decode_scored(layer, shape, cache, a["q"], ctx, 32, a["si"], a["s"], q)
+
+
+def _shared(layer=None, shape=None, cache=None, q=FAKE, ctx=FAKE, ns=4, nq=1, maxc=500, cu=FAKE, sl=FAKE, ng=2, top=200,
+            ws=FAKE, wsb=1 << 40, out=FAKE):
+    return hswa.load().hswa_decode_shared(layer or _full(), ctypes.byref(shape or _shape()),
+                                          ctypes.byref(cache or _cache()), q, ctx, ns, nq, maxc, cu, sl, ng, top, ws, wsb,
+                                          out, None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(ns=0, ng=0), OK),
+    (dict(layer=hswa._Layer(7, 1)), INVALID), (dict(layer=hswa._Layer(hswa.HSWA_LAYER_SWA, 0)), INVALID),
+    (dict(shape=_shape(d=64)), UNSUPPORTED), (dict(shape=_shape(hq=63)), INVALID), (dict(shape=_shape(pg=8)), UNSUPPORTED),
+    (dict(ns=-1, ng=0), INVALID), (dict(nq=0), INVALID), (dict(nq=65), INVALID), (dict(maxc=0), INVALID),
+    (dict(ng=-1), INVALID), (dict(ng=5), INVALID), (dict(top=-1), INVALID),
+    (dict(cu=None), INVALID), (dict(sl=None), INVALID),
+    (dict(cache=_cache(7)), CAPACITY), (dict(cache=_cache(pages=0)), INVALID), (dict(wsb=1000), CAPACITY),
+    (dict(q=None), INVALID), (dict(ctx=None), INVALID), (dict(out=None), INVALID), (dict(ws=None), INVALID),
+    # without a group, or a tile that could be shared, the refusals of decode_multi
+    (dict(ng=0, cu=None, sl=None, q=None), INVALID), (dict(top=63, wsb=0, ws=None), INVALID),
+    (dict(ng=0, cache=_cache(7)), CAPACITY), (dict(ng=0, nq=65), INVALID),
+])
+def test_decode_shared_refusals(kw, code):
+    assert _shared(**kw) == code
+
+
+def test_decode_shared_workspace():
+    sh = hswa.Shape(64, 8)
+    need = hswa.decode_shared_workspace_bytes(sh, 4, 1, 5000, 2, 1000)
+    assert need > hswa.decode_workspace_bytes(sh, 4, 5000)
+    assert hswa.decode_shared_workspace_bytes(sh, 4, 2, 5000, 0, 1000) == hswa.decode_multi_workspace_bytes(sh, 4, 2, 5000)
+    assert hswa.decode_shared_workspace_bytes(sh, 4, 1, 5000, 2, 63) == hswa.decode_workspace_bytes(sh, 4, 5000)
+    for a in ((0, 1, 100, 0, 0), (2, 0, 100, 1, 64), (2, 65, 100, 1, 64), (2, 1, 0, 1, 64), (2, 1, 100, 3, 64),
+              (2, 1, 100, -1, 64), (2, 1, 100, 1, -1)):
+        assert hswa.decode_shared_workspace_bytes(sh, *a) == 0
+
+
+def test_decode_shared_binding_refusals():
+    shape, cache, layer = hswa.Shape(4, 2, 128, 16), _cpu_cache(), hswa.Layer.full()
+    q, ctx = torch.zeros((2, 4, 128), dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32)
+    i = torch.zeros(2, dtype=torch.int32)
+    for bad in (dict(q=q[0]), dict(q=q[:1]), dict(cu=i[:1]), dict()):
+        a = dict(q=q, cu=i) | bad
+        with pytest.raises(ValueError):
+            hswa.decode_shared(layer, shape, cache, a["q"], ctx, 32, a["cu"], i[:1], 16, q)
