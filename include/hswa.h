@@ -406,7 +406,8 @@ hswa_status hswa_decode_scored(hswa_layer layer, const hswa_shape *shape, const 
  * [0, max_context_len], budgets to [0, kept_stride]). kept_out: device int32
  * [ns][Hkv][kept_stride], receives the kept positions in increasing order;
  * scores_out: device fp32 [ns][Hkv][scores_out_stride >= kept_stride] or NULL,
- * receives their scores; it must not overlap `scores`. Entries from K_b on, and
+ * receives their scores. No output may overlap an input (new_lens_out is not
+ * context_lens, scores_out not scores). Entries from K_b on, and
  * slots of `dst` from K_b on, are left as they were. new_lens_out: device int32
  * [ns], receives K_b. A kept position whose page id is not in the pool is
  * stored as a zero key and value, a slot whose page id is not is not stored.

@@ -129,16 +129,21 @@ DecodeGeometry decode_geometry(const hswa_shape *sh, int32_t ns, int32_t max_ctx
   return g;
 }
 
-// Scored decode: the split partials, then the rows' log-sum-exps.
+// Scored decode: the split partials, then all scores or the rows' log-sum-exps.
 struct ScoredGeometry {
   DecodeGeometry d;
+  bool keep;
+  int64_t max_chunks;
   size_t total_bytes;
 };
 
 ScoredGeometry scored_geometry(const hswa_shape *sh, int32_t ns, int32_t max_ctx, int32_t nq) {
   ScoredGeometry g{};
   g.d = decode_geometry(sh, ns, max_ctx, nq, true);
-  g.total_bytes = g.d.total_bytes + align_up((size_t)ns * nq * sh->num_q_heads * sizeof(float), 256);
+  const size_t rows = (size_t)ns * nq * sh->num_q_heads;
+  g.keep = nq * (sh->num_q_heads / sh->num_kv_heads) <= hswa::kKeepColumns;
+  g.max_chunks = ((int64_t)max_ctx + 31) / 32;
+  g.total_bytes = g.d.total_bytes + align_up(rows * sizeof(float) * (g.keep ? (size_t)g.max_chunks * 32 : 1), 256);
   return g;
 }
 
@@ -518,7 +523,8 @@ hswa_status hswa_decode_scored(hswa_layer layer, const hswa_shape *shape, const 
   char *ws = static_cast<char *>(workspace);
   p.d.ws_o = reinterpret_cast<float *>(ws);
   p.d.ws_lse = reinterpret_cast<float *>(ws + geo.d.o_bytes);
-  p.d.row_lse = reinterpret_cast<float *>(ws + geo.d.total_bytes);
+  (geo.keep ? p.d.ws_s : p.d.row_lse) = reinterpret_cast<float *>(ws + geo.d.total_bytes);
+  p.d.max_chunks = geo.max_chunks;
   p.scores_in = scores_in;
   p.scores_out = scores_out;
   p.stride = score_stride;
@@ -547,6 +553,8 @@ hswa_status hswa_kv_evict(hswa_layer layer, const hswa_shape *shape, const hswa_
   if (ns == 0) return HSWA_OK;
   if (!scores || !context_lens || !budgets || !kept_out || !new_lens_out || scores_out == scores)
     return HSWA_ERR_INVALID_ARG;
+  // (each KV head's workgroup reads the lengths and budgets, one of them writes the new lengths)
+  if (new_lens_out == context_lens || new_lens_out == budgets) return HSWA_ERR_INVALID_ARG;
   p.scores = scores;
   p.ctx_lens = context_lens;
   p.budgets = budgets;

@@ -56,11 +56,17 @@ __device__ __forceinline__ u32x4 ldnt128(const void *p) {
 //            probabilities in fp32, not as rounded to bf16 for the PV product
 //            (the log-sum-exp then gives each key's weight to fp32), every row
 //            in partials
+//   kKept    kScored that also stores the scores (in exp2 units)
 //   kSuffix  decode_shared.hip: split spans over the keys from start[b] on, a
 //            row with keys before that in partials
-enum DecodeMode { kDecode, kScored, kSuffix };
+enum DecodeMode { kDecode, kScored, kKept, kSuffix };
+constexpr bool scored(int mode) { return mode == kScored || mode == kKept; }
 
 constexpr int kChunk = 32;
+// Fourth word of a gfx9 buffer resource for raw accesses (32-bit data format, no
+// swizzle, no index stride), and the cache policy (SC1) that writes through L2.
+constexpr int kBufferWord3 = 0x00020000;
+constexpr int kWriteThrough = 16;
 constexpr int kCols = 16;  // query heads per item (MFMA columns)
 constexpr int kMergeThreads = 256;
 // Up to this many rows a merged row has a workgroup of its own: with one wave
@@ -154,6 +160,7 @@ struct ChunkPages {
 // range, and combine their partial softmax states through LDS (still one
 // pass: no workspace and no second kernel).
 constexpr int kWaves = 4;
+constexpr int kKeepPieces = 2304;  // 16-byte pieces of kept scores a wave holds in LDS (a workgroup: 144 of 160 KiB)
 template <bool kSplit>
 constexpr int kCoop = kSplit ? 1 : kWaves;  // waves that share one item
 
@@ -170,6 +177,7 @@ void decode_kernel(DecodeParams p) {
   const PoolView &pv = p.pool;
   const int lane = threadIdx.x & (kWave - 1);
   const int wid = threadIdx.x >> 6;  // wave of the workgroup
+  [[maybe_unused]] __shared__ f32x4 s_keep[kWaves][kKeepPieces];  // (kKept)
   const int r = lane & 15, q = lane >> 4;
   const int hkv = p.hkv;
   const int shift = pv.pg_shift;
@@ -249,7 +257,7 @@ void decode_kernel(DecodeParams p) {
       const int64_t seg = pb + (int64_t)gy * nch;
       c_hi = (int)min((int64_t)nch, c_lo + (u1 - u));
       piece = (int)((seg + c_lo) / per - seg / per);
-      whole = kMode != kScored && c_lo == 0 && c_hi == nch;
+      whole = !scored(kMode) && c_lo == 0 && c_hi == nch;
     }
     {
       const int g = gy / hchunks;
@@ -378,6 +386,27 @@ void decode_kernel(DecodeParams p) {
         for (int dt = 0; dt < 8; ++dt) ch.v[dt] = ldnt128(vbase + voff + dt * vstep);
       };
 
+      // kKept: the scores of the last `kept` chunks, in LDS until they fill it, so
+      // that they go out in long runs: their bytes are a sixteenth of those read,
+      // but writes between the reads cost HBM far more than that. 16 x 64K, 64 / 8
+      // heads, us: 610 without the stores, 807 with a chunk's 1 KiB at a time, 797
+      // in runs of 16 KiB, 775 of 36 KiB, NNN written through past L2 (a line
+      // held there is evicted in between some later reads).
+      int kept = 0;
+      int64_t kept_to = 0;  // where the next run goes, in 16-byte pieces
+      if constexpr (kMode == kKept) kept_to = uni64((((int64_t)b * hkv + g) * p.max_chunks + c_lo) * ncols * 8);
+      auto store_kept = [&]() {
+        __builtin_amdgcn_wave_barrier();
+        const int n = kept * ncols * 8;
+        const __amdgpu_buffer_rsrc_t rs =
+            __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<f32x4 *>(p.ws_s) + kept_to, 0, n * 16, kBufferWord3);
+        for (int i = lane; i < n; i += kWave)
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, s_keep[wid][i]), rs, i * 16, 0, kWriteThrough);
+        kept_to += n;
+        kept = 0;
+        __builtin_amdgcn_wave_barrier();
+      };
+
       // QK^T and the online softmax of one chunk: returns P^T packed as bf16 and
       // leaves the key mask in `keep`. The running maximum of a column is only
       // raised when one of its scores exceeds it by more than 2^8 in exp2 units
@@ -417,6 +446,13 @@ void decode_kernel(DecodeParams p) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) s[i] = (sk >> i) & 1u ? s[i] : -INFINITY;
           }
+          if constexpr (kMode == kKept) {
+            if (colv[cg]) {
+              f32x4 *dst = s_keep[wid] + kept * ncols * 8 + (16 * cg + r) * 4 + q;
+              dst[0] = f32x4{s[0], s[1], s[2], s[3]} * c2;
+              dst[4 * ncols] = f32x4{s[4], s[5], s[6], s[7]} * c2;
+            }
+          }
           const float lmax = max8(s) * c2;
           if (__builtin_amdgcn_ballot_w64(lmax > m[cg] + kRescaleLog2) != 0) {
             const float cmax = max_xor32(max_xor16(lmax));
@@ -433,7 +469,7 @@ void decode_kernel(DecodeParams p) {
           for (int i = 0; i < 8; ++i) pr[i] = fast_exp2(fmaf(s[i], c2, -mc));
 #pragma unroll
           for (int j = 0; j < 4; ++j) pf[cg][j] = pack_bf16x2(pr[2 * j], pr[2 * j + 1]);
-          if constexpr (kMode == kScored) {
+          if constexpr (scored(kMode)) {
             lsum[cg] += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
           } else {
 #pragma unroll
@@ -455,6 +491,8 @@ void decode_kernel(DecodeParams p) {
         for (int dt = 0; dt < 8; ++dt)
 #pragma unroll
           for (int cg = 0; cg < kCGd; ++cg) acc[cg][dt] = mfma16x16x32(ch.v[dt], pf[cg], acc[cg][dt]);
+        if constexpr (kMode == kKept)
+          if (++kept * ncols * 8 + ncols * 8 > kKeepPieces) store_kept();
       };
 
       {
@@ -599,6 +637,8 @@ void decode_kernel(DecodeParams p) {
         }
       }
 
+      if constexpr (kMode == kKept) store_kept();
+
       // Lane holds O^T[d = 16 dt + 4 q + i][column r of group cg], relative to
       // its column maximum m.
       if constexpr (!kSplit) {
@@ -701,13 +741,13 @@ void decode_kernel(DecodeParams p) {
 // dims a lane (16-byte loads, 16 pieces in flight a step). kScored: also writes
 // the row's log-sum-exp (+infinity for a row that sees no key).
 template <int kRowWaves, int kMode = kDecode>
-__global__ __launch_bounds__(kMergeThreads) void decode_merge_kernel(DecodeParams p) {
+__device__ __forceinline__ void merge_rows(const DecodeParams &p, int64_t block) {
   constexpr int kMergeWaves = kMergeThreads / kWave;
   static_assert(kRowWaves == 1 || kRowWaves == kMergeWaves, "a row has one wave or its workgroup");
   const int lane = threadIdx.x & (kWave - 1);
   const int wid = uni((int)(threadIdx.x / kWave));
   const int rw = kRowWaves == 1 ? 0 : wid;  // wave of the row
-  const int64_t idx = (int64_t)blockIdx.x * (kMergeWaves / kRowWaves) + (kRowWaves == 1 ? wid : 0);
+  const int64_t idx = block * (kMergeWaves / kRowWaves) + (kRowWaves == 1 ? wid : 0);
   if (idx >= (int64_t)p.ns * p.nq * p.hq) return;
   const int b = (int)(idx / ((int64_t)p.nq * p.hq));
   const int ctx = min(p.ctx_lens[b], p.max_ctx);
@@ -738,7 +778,7 @@ __global__ __launch_bounds__(kMergeThreads) void decode_merge_kernel(DecodeParam
   const int nch = (ctx + kChunk - 1) / kChunk;
   const int64_t seg = pb + (int64_t)(g * hchunks + col / p.item_cols) * nch;
   const int nsplit = (int)((seg + nch - 1) / per - seg / per) + 1;
-  if (kMode != kScored && nsplit == 1) return;  // one piece: the decode kernel wrote the row
+  if (!scored(kMode) && nsplit == 1) return;  // one piece: the decode kernel wrote the row
   const float *lse = p.ws_lse + idx * p.max_splits;
   float mx = -INFINITY;
   for (int s = lane; s < nsplit; s += kWave) mx = fmaxf(mx, lse[s]);
@@ -804,6 +844,11 @@ __global__ __launch_bounds__(kMergeThreads) void decode_merge_kernel(DecodeParam
     w2[1] = pack_bf16x2(o[2] * inv, o[3] * inv);
     *dst = w2;
   }
+}
+
+template <int kRowWaves, int kMode = kDecode>
+__global__ __launch_bounds__(kMergeThreads) void decode_merge_kernel(DecodeParams p) {
+  merge_rows<kRowWaves, kMode>(p, blockIdx.x);
 }
 
 // Waves of the split kernel that the current device holds at once (workgroups per CU from

@@ -2,16 +2,26 @@
 // in KV head g is the sum over the call's queries and g's query heads h of
 //     exp2(scale log2(e) <q_h, k_j> - lse_h),
 // lse_h the row's log2 sum-exp over all its keys. That is known only once the
-// whole context has been read, so there are three kernels: the split decode
-// (decode_kernels.h, row sums in fp32), the merge of its partials, which also
-// leaves the rows' log-sum-exps, and the weights, which read K a second time and
-// form the scores anew on the matrix cores.
+// whole context has been read, so the weights come after the split decode
+// (decode_kernels.h, row sums in fp32), in one of two ways:
+//   up to kKeepColumns columns (queries x heads of a KV head): the decode also
+//     stores the scores in fp32, and one more kernel merges the rows and turns
+//     the scores into weights. A column costs 8 bytes a key (written and read),
+//     a key's K and V 512.
+//   more: the merge leaves the rows' log-sum-exps and a third kernel reads K a
+//     second time (256 bytes a key, whatever the columns) and forms the scores
+//     anew on the matrix cores.
+#include <algorithm>
+
 #include "decode_kernels.h"
 
 namespace hswa {
 namespace {
 
-constexpr int kScoreThreads = 256;
+constexpr int kScoreThreads = kMergeThreads;
+constexpr int kKeptKeys = 4 * kScoreThreads;  // keys of a workgroup, from kept scores
+constexpr int kMaxScoreGrid = 1 << 20;
+static_assert(kKeepColumns >= kCols, "one column group's scores are always kept");
 constexpr int kWaveChunks = 4;  // 32-key chunks a wave holds at once
 constexpr int kScoreKeys = kScoreThreads / kWave * kWaveChunks * kChunk;  // keys of a workgroup
 
@@ -30,19 +40,19 @@ __device__ __forceinline__ float row_sum16(float x) {
 // Weights of 512 keys of a (sequence, KV head), 128 a wave. kOnePage: a
 // 32-key chunk lies in one page.
 template <bool kOnePage>
-__global__ __launch_bounds__(kScoreThreads) void score_kernel(ScoredParams sp) {
+__global__ __launch_bounds__(kScoreThreads) __attribute__((amdgpu_waves_per_eu(2))) void score_kernel(ScoredParams sp) {
   const DecodeParams &p = sp.d;
   const PoolView &pv = p.pool;
   const int lane = threadIdx.x & (kWave - 1), wave = uni((int)(threadIdx.x / kWave));
   const int r = lane & 15, q = lane >> 4;
-  const int tiles = (p.max_ctx + kScoreKeys - 1) / kScoreKeys;
-  const int64_t rows = (int64_t)p.ns * p.hkv;
-  const int64_t bg = blockIdx.x % rows;
-  const int tile = (int)(blockIdx.x / rows);
+  const int64_t rows = (int64_t)p.ns * p.hkv, items = rows * ((p.max_ctx + kScoreKeys - 1) / kScoreKeys);
+  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+  const int64_t bg = item % rows;
+  const int tile = (int)(item / rows);
   const int b = (int)(bg / p.hkv), g = (int)(bg - (int64_t)b * p.hkv);
   const int ctx = min(p.ctx_lens[b], p.max_ctx);
   const int k0 = tile * kScoreKeys + wave * kWaveChunks * kChunk;  // this wave's first key
-  if (tile >= tiles || k0 >= ctx) return;
+  if (k0 >= ctx) continue;
   const int pos0 = ctx - p.nq;  // the first query's position
   const int ncols = p.nq * p.group;
 
@@ -115,37 +125,117 @@ __global__ __launch_bounds__(kScoreThreads) void score_kernel(ScoredParams sp) {
       sp.scores_out[at] = (sp.scores_in ? sp.scores_in[at] : 0.f) + mine;
     }
   }
+  }
 }
 
-template <int kCGd>
+// The rows' merge (the first `merge_blocks` workgroups), and the weights of 1024
+// keys of a (sequence, KV head) from the scores that the decode stored, four
+// keys a thread.
+template <int kRowWaves>
+__global__ __launch_bounds__(kScoreThreads) void scored_finish_kernel(ScoredParams sp) {
+  const DecodeParams &p = sp.d;
+  if (blockIdx.x < (unsigned)sp.merge_blocks) {
+    merge_rows<kRowWaves, kKept>(p, blockIdx.x);
+    return;
+  }
+  __shared__ float s_lse[kKeepColumns];
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = uni((int)(tid / kWave));
+  const int ncols = p.nq * p.group;
+  int64_t total = 0;  // chunks of all sequences: the spans' length (as in the decode kernel)
+  for (int s0 = 0; s0 < p.ns; s0 += kWave) total += wave_sum64(seq_chunks(p, s0 + lane));
+  total = uni64(total) * p.hkv;
+  const int64_t per = max((int64_t)(p.split_len / kChunk), (total + p.span_waves - 1) / p.span_waves);
+  const int64_t rows = (int64_t)p.ns * p.hkv, items = rows * ((p.max_ctx + kKeptKeys - 1) / kKeptKeys);
+  const int64_t step = (int64_t)gridDim.x - sp.merge_blocks;
+  for (int64_t item = (int64_t)blockIdx.x - sp.merge_blocks; item < items; item += step) {
+    const int64_t bg = item % rows;
+    const int b = (int)(bg / p.hkv), g = (int)(bg - (int64_t)b * p.hkv);
+    const int ctx = min(p.ctx_lens[b], p.max_ctx);
+    const int k0 = (int)(item / rows) * kKeptKeys;
+    if (k0 >= ctx) continue;  // (the same for every thread)
+    int64_t before = 0;
+    for (int s0 = 0; s0 < b; s0 += kWave) before += wave_sum64(s0 + lane < b ? seq_chunks(p, s0 + lane) : 0);
+    const int nch = (ctx + kChunk - 1) / kChunk;
+    const int64_t seg = uni64(before) * p.hkv + (int64_t)g * nch;
+    const int pieces = (int)((seg + nch - 1) / per - seg / per) + 1;
+    __syncthreads();  // (s_lse of the item before has been read)
+    for (int c = wave; c < ncols; c += kScoreThreads / kWave) {
+      const int qi = c / p.group;
+      const int64_t row = ((int64_t)b * p.nq + qi) * p.hq + (int64_t)g * p.group + (c - qi * p.group);
+      const float *lse = p.ws_lse + row * p.max_splits;
+      float mx = -INFINITY;
+      for (int s = lane; s < pieces; s += kWave) mx = fmaxf(mx, lse[s]);
+#pragma unroll
+      for (int off = 1; off < kWave; off <<= 1) mx = fmaxf(mx, __shfl_xor(mx, off, kWave));
+      float sum = 0.f;
+      for (int s = lane; s < pieces; s += kWave) sum += fast_exp2(lse[s] - mx);
+#pragma unroll
+      for (int off = 1; off < kWave; off <<= 1) sum += __shfl_xor(sum, off, kWave);
+      // (a row that sees no key has scores of -infinity: weight 0 under any finite or +infinite sum)
+      if (lane == 0) s_lse[c] = mx == -INFINITY ? INFINITY : mx + __log2f(sum);
+    }
+    __syncthreads();
+    const int j = k0 + 4 * tid;
+    if (j < ctx) {
+      const int o = (j & (kChunk - 1)) >> 2;  // (see hswa_launch.h for the order)
+      const f32x4 *src = reinterpret_cast<const f32x4 *>(p.ws_s) + (bg * p.max_chunks + (j >> 5)) * ncols * 8 +
+                         (o & 1) * 4 * ncols + (o >> 1);
+      f32x4 w = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+      for (int c = 0; c < ncols; ++c) {
+        const f32x4 s = src[4 * c];
+        const float l = s_lse[c];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] += fast_exp2(s[i] - l);
+      }
+      const int64_t at = bg * sp.stride + j;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (j + i < ctx) sp.scores_out[at + i] = (sp.scores_in ? sp.scores_in[at + i] : 0.f) + w[i];
+    }
+  }
+}
+
+// The split decode, with `kMode`, and what follows it.
+template <int kCGd, int kMode>
 hipError_t launch_cg(const ScoredParams &p0, hipStream_t stream) {
   ScoredParams sp = p0;
   DecodeParams &p = sp.d;
   p.item_cols = kCols * kCGd;
   const bool one_page = p.pool.pg_shift >= 5;
-  hipError_t e = one_page ? resident_split_waves<true, kCGd, kScored>(p.span_waves)
-                          : resident_split_waves<false, kCGd, kScored>(p.span_waves);
+  hipError_t e = one_page ? resident_split_waves<true, kCGd, kMode>(p.span_waves)
+                          : resident_split_waves<false, kCGd, kMode>(p.span_waves);
   if (e != hipSuccess) return e;
-  const dim3 grid((unsigned)(p.span_waves / kWaves)), block(kWave * kWaves);
-  e = one_page ? launch_kernel(decode_kernel<true, true, kCGd, kScored>, grid, block, stream, p)
-               : launch_kernel(decode_kernel<true, false, kCGd, kScored>, grid, block, stream, p);
+  const dim3 grid((unsigned)(p.span_waves / kWaves)), block(kWave * kWaves), threads(kScoreThreads);
+  e = one_page ? launch_kernel(decode_kernel<true, true, kCGd, kMode>, grid, block, stream, p)
+               : launch_kernel(decode_kernel<true, false, kCGd, kMode>, grid, block, stream, p);
   if (e != hipSuccess) return e;
   const int64_t rows = (int64_t)p.ns * p.nq * p.hq;
   constexpr int per_block = kMergeThreads / kWave;
-  e = rows <= kWideMergeRows
-          ? launch_kernel(decode_merge_kernel<per_block, kScored>, dim3((unsigned)rows), dim3(kMergeThreads), stream, p)
-          : launch_kernel(decode_merge_kernel<1, kScored>, dim3((unsigned)((rows + per_block - 1) / per_block)),
-                          dim3(kMergeThreads), stream, p);
-  if (e != hipSuccess) return e;
-  const int64_t items = (int64_t)p.ns * p.hkv * ((p.max_ctx + kScoreKeys - 1) / kScoreKeys);
-  return one_page ? launch_kernel(score_kernel<true>, dim3((unsigned)items), dim3(kScoreThreads), stream, sp)
-                  : launch_kernel(score_kernel<false>, dim3((unsigned)items), dim3(kScoreThreads), stream, sp);
+  const bool wide = rows <= kWideMergeRows;
+  const dim3 merge((unsigned)(wide ? rows : (rows + per_block - 1) / per_block));
+  const int64_t keys = kMode == kKept ? kKeptKeys : kScoreKeys;
+  const dim3 items((unsigned)std::min<int64_t>((int64_t)p.ns * p.hkv * ((p.max_ctx + keys - 1) / keys), kMaxScoreGrid));
+  if constexpr (kMode == kKept) {
+    sp.merge_blocks = merge.x;
+    const dim3 both(merge.x + items.x);
+    return wide ? launch_kernel(scored_finish_kernel<per_block>, both, threads, stream, sp)
+                : launch_kernel(scored_finish_kernel<1>, both, threads, stream, sp);
+  } else {
+    e = wide ? launch_kernel(decode_merge_kernel<per_block, kScored>, merge, threads, stream, p)
+             : launch_kernel(decode_merge_kernel<1, kScored>, merge, threads, stream, p);
+    if (e != hipSuccess) return e;
+    return one_page ? launch_kernel(score_kernel<true>, items, threads, stream, sp)
+                    : launch_kernel(score_kernel<false>, items, threads, stream, sp);
+  }
 }
 
 }  // namespace
 
 hipError_t launch_decode_scored(const ScoredParams &p, hipStream_t stream) {
-  return p.d.nq * p.d.group > kCols ? launch_cg<2>(p, stream) : launch_cg<1>(p, stream);
+  const int columns = p.d.nq * p.d.group;
+  if (columns <= kCols) return launch_cg<1, kKept>(p, stream);
+  return columns <= kKeepColumns ? launch_cg<2, kKept>(p, stream) : launch_cg<2, kScored>(p, stream);
 }
 
 }  // namespace hswa

@@ -65,6 +65,10 @@ struct DecodeParams {
   // stores the token (k_new / v_new) in its slot and takes its key from them
   int32_t split_append;
   float *row_lse;             // scored decode: [ns * nq * Hq], the rows' log2 sum-exps
+  // or all scores in exp2 units, [ns][Hkv][max_chunks][2][nq * group][4][4]: key k of a 32-key
+  // chunk at half k / 4 % 2, place k / 8, element k % 4
+  float *ws_s;
+  int64_t max_chunks;         // 32-key chunks of max_ctx
   const int32_t *start;       // suffix decode: [ns], first key (a multiple of 32) of each sequence
   const int64_t *suffix_per;  // and the chunks of a span
 };
@@ -137,11 +141,13 @@ struct EvictParams {
 };
 
 // Decode that also adds every key's attention weight to a score (decode_scored.hip).
+constexpr int kKeepColumns = 32;  // up to this many (query, head) columns of a KV head the scores are stored
 struct ScoredParams {
-  DecodeParams d;          // split (max_splits > 1), with row_lse
+  DecodeParams d;          // split (max_splits > 1), with ws_s or row_lse
   const float *scores_in;  // [ns][Hkv][stride], or null for zeros; may be scores_out
   float *scores_out;
   int64_t stride;
+  int64_t merge_blocks;    // workgroups that merge rows (set at launch)
 };
 
 hipError_t launch_kv_append(const AppendParams &p, hipStream_t stream);

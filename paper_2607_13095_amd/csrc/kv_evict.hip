@@ -24,9 +24,12 @@ constexpr int kSelectThreads = 1024;
 constexpr int kSelectWaves = kSelectThreads / kWave;
 constexpr int kDigit = 11;  // bits of a digit: three passes over 32-bit scores
 constexpr int kBins = 1 << kDigit;
-constexpr int kCopyThreads = 256;
-constexpr int kSlots = 32;  // slots of the new pages per workgroup of the move
-constexpr int kMaxCopyGrid = 1 << 20;
+constexpr int kBatch = 16;
+constexpr int kCopies = 4;  // of the histogram, for lanes that meet in a bin
+constexpr int kMoveThreads = 256;
+constexpr int kSlots = 32;        // slots of the new pages per workgroup of the move
+constexpr int kStageBlocks = 4;   // V blocks a wave holds in LDS (a power of two)
+constexpr int kMaxMoveGrid = 1 << 20;
 
 // What a sequence keeps, by count: its first and last keys and those picked by
 // score out of [sinks, len - recent).
@@ -50,11 +53,15 @@ __device__ __forceinline__ uint32_t score_key(float s) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+// kPer: scores that a thread holds in registers, 64 positions of a wave apart; 0:
+// any number, read again for each of the five passes, kBatch loads at a time
+// (one at a time a pass over 58K scores took 20 us; 64 held spilled).
+template <int kPer>
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictParams p) {
-  __shared__ uint32_t hist[kBins];
+  __shared__ uint32_t hist[kBins * kCopies];
   __shared__ uint32_t wsum[2][kSelectWaves];
-  __shared__ uint32_t found[2];
-  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+  __shared__ uint32_t found[3];
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int b = (int)(blockIdx.x / p.hkv), g = (int)(blockIdx.x - (int64_t)b * p.hkv);
   const Keep n = keep_of(p, b);
   if (g == 0 && tid == 0) p.new_lens[b] = n.keep;
@@ -67,29 +74,71 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictParam
     if (out) out[slot] = scores[pos];
   };
   const int lo = n.sinks, hi = n.len - n.recent;
+  // this wave's stretch of the positions that are picked from: groups of 64
+  const int groups = (hi - lo + kSelectWaves * kWave - 1) / (kSelectWaves * kWave);
+  const int w0 = min(hi, lo + wave * groups * kWave), w1 = min(hi, w0 + groups * kWave);
+  float held[kPer > 0 ? kPer : 1];
+  const bool choose = n.pick > 0 && n.pick < hi - lo;
+  if (kPer > 0 && choose) {
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      const int i = w0 + e * kWave + lane;
+      held[e] = i < w1 ? scores[i] : 0.f;
+    }
+  }
   for (int i = tid; i < n.sinks; i += kSelectThreads) emit(i, i);
   for (int i = tid; i < n.recent; i += kSelectThreads) emit(n.keep - n.recent + i, hi + i);
-  if (n.pick == 0) return;
-  if (n.pick == hi - lo) {
+  if (!choose) {
     for (int i = tid; i < n.pick; i += kSelectThreads) emit(lo + i, lo + i);
     return;
   }
+  // f(position, key, whether there is one) for 64 positions of the stretch at a time
+  auto each = [&](auto f) __attribute__((always_inline)) {
+    if constexpr (kPer > 0) {
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) {
+        if (w0 + e * kWave >= w1) break;  // (the same for the wave)
+        const int i = w0 + e * kWave + lane;
+        f(i, score_key(held[e]), held[e], i < w1);
+      }
+    } else {
+      for (int i0 = w0; i0 < w1; i0 += kBatch * kWave) {
+        float s[kBatch];
+#pragma unroll
+        for (int e = 0; e < kBatch; ++e) {
+          const int i = i0 + e * kWave + lane;
+          s[e] = i < w1 ? scores[i] : 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < kBatch; ++e) {
+          if (i0 + e * kWave >= w1) break;
+          const int i = i0 + e * kWave + lane;
+          f(i, score_key(s[e]), s[e], i < w1);
+        }
+      }
+    }
+  };
   // The pick-th highest key, digit by digit: `top` is what is known of it, of
   // the keys that share `top` the `need` highest stay.
   uint32_t top = 0, known = 0, need = n.pick;
   bool ties = true;  // whether only some of the keys equal to `top` stay
+#pragma unroll 1
   for (int shift = 32 - kDigit;; shift = max(shift - kDigit, 0)) {
-    const uint32_t digit = known == 0xFFFFFFFFu << (32 - 2 * kDigit) ? (1u << (32 - 2 * kDigit)) - 1 : kBins - 1;
-    for (int i = tid; i < kBins; i += kSelectThreads) hist[i] = 0;
+    const uint32_t digit = shift == 0 ? (1u << (32 - 2 * kDigit)) - 1 : kBins - 1;
+    for (int i = tid; i < kBins * kCopies; i += kSelectThreads) hist[i] = 0;
     __syncthreads();
-    for (int i = lo + tid; i < hi; i += kSelectThreads) {
-      const uint32_t k = score_key(scores[i]);
-      if ((k & known) == top) atomicAdd(&hist[(k >> shift) & digit], 1u);
-    }
+    each([&](int, uint32_t k, float, bool in) {
+      if (in && (k & known) == top) atomicAdd(&hist[((k >> shift) & digit) * kCopies + (lane & (kCopies - 1))], 1u);
+    });
     __syncthreads();
     // the bins from the highest down, two a thread: where the count reaches `need`
     const int hb = kBins - 1 - 2 * tid;
-    const uint32_t c0 = hist[hb], c1 = hist[hb - 1];
+    uint32_t c0 = 0, c1 = 0;
+#pragma unroll
+    for (int c = 0; c < kCopies; ++c) {
+      c0 += hist[hb * kCopies + c];
+      c1 += hist[(hb - 1) * kCopies + c];
+    }
     uint32_t s = c0 + c1;
 #pragma unroll
     for (int off = 1; off < kWave; off <<= 1) {
@@ -104,27 +153,24 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictParam
       const bool first = need <= before + c0;
       found[0] = first ? hb : hb - 1;
       found[1] = first ? before : before + c0;
+      found[2] = first ? c0 : c1;
     }
     __syncthreads();
-    const uint32_t d = found[0];
     need -= found[1];
-    top |= d << shift;
+    top |= found[0] << shift;
     known |= digit << shift;
-    ties = hist[d] > need;
-    __syncthreads();  // (hist, wsum and found are written again)
-    if (shift == 0 || !ties) break;
+    ties = found[2] > need;
+    if (shift == 0 || !ties) break;  // (hist is cleared before found is written again, a barrier later)
   }
   // Kept: keys above `top`, and of those equal to it (in its known digits) all,
   // or the first `need` by position.
-  const int stretch = ((hi - lo + kSelectWaves * kWave - 1) / (kSelectWaves * kWave)) * kWave;
-  const int w0 = min(hi, lo + wave * stretch), w1 = min(hi, w0 + stretch);
   uint32_t above = 0, equal = 0;
-  for (int i0 = w0; i0 < w1; i0 += kWave) {
-    const int i = i0 + lane;
-    const uint32_t k = i < w1 ? score_key(scores[i]) & known : 0;
-    above += __popcll(__ballot(i < w1 && k > top));
-    equal += __popcll(__ballot(i < w1 && k == top));
-  }
+  each([&](int, uint32_t key, float, bool in) {
+    const uint32_t k = key & known;
+    above += __popcll(__ballot(in && k > top));
+    equal += __popcll(__ballot(in && k == top));
+  });
+  __syncthreads();  // (wsum has been read)
   if (lane == 0) {
     wsum[0][wave] = above;
     wsum[1][wave] = equal;
@@ -138,75 +184,134 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictParam
   if (!ties) need = 0xFFFFFFFFu;
   slot += n.sinks + min(eq, need);
   const uint64_t below = ((uint64_t)1 << lane) - 1;
-  for (int i0 = w0; i0 < w1; i0 += kWave) {
-    const int i = i0 + lane;
-    const uint32_t k = i < w1 ? score_key(scores[i]) & known : 0;
-    const uint64_t same = __ballot(i < w1 && k == top);
-    const bool keep = i < w1 && (k > top || (k == top && eq + __popcll(same & below) < need));
+  each([&](int i, uint32_t key, float score, bool in) {
+    const uint32_t k = key & known;
+    const uint64_t same = __ballot(in && k == top);
+    const bool keep = in && (k > top || (k == top && eq + __popcll(same & below) < need));
     const uint64_t mine = __ballot(keep);
-    if (keep) emit((int)slot + __popcll(mine & below), i);
+    if (keep) {
+      const int to = (int)slot + __popcll(mine & below);
+      kept[to] = i;
+      if (out) out[to] = score;
+    }
     slot += __popcll(mine);
     eq += __popcll(same);
-  }
+  });
 }
 
 // Page of position j of sequence b, -1 if the table has none.
-__device__ __forceinline__ int64_t page_of(const PoolView &pv, int b, int j) {
+__device__ __forceinline__ int page_of(const PoolView &pv, int b, int j) {
   const int lp = j >> pv.pg_shift;
   if (lp >= pv.stride) return -1;
   const int64_t v = pv.table[(int64_t)b * pv.stride + lp];
-  return v >= 0 && v < pv.num_pages ? v : -1;
+  return v >= 0 && v < pv.num_pages ? (int)v : -1;
 }
 
-__global__ __launch_bounds__(kCopyThreads) void evict_move_kernel(EvictParams p) {
-  __shared__ int64_t from[kSlots];  // element offset of each key's page-head and its offset in the page, -1: none
-  __shared__ int off[kSlots];
-  const int tid = threadIdx.x;
+// 32 slots of the new pages. K moves in 16-byte pieces (8 dims of a key). V is
+// stored with a block's keys side by side, so a kept key is 2 bytes here and
+// there: each wave takes 32 dims, loads whole rows of the blocks that hold kept
+// keys (kStageBlocks at a time, in LDS) and picks from them the 16 slots of a
+// lane's dim. kB: keys of a block (16 for 16-key pages, else 32).
+template <int kB>
+__global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictParams p) {
+  constexpr int kDims = kHeadDim / (kMoveThreads / kWave);  // dims of a wave
+  constexpr int kRow = 2 * kB / 16;                         // 16-byte pieces of a block's row
+  constexpr int kPad = kRow + 1;                            // and of a row in LDS
+  constexpr int kLoads = kDims * kRow / kWave;              // pieces of a block for a lane
+  static_assert(kDims * 2 == kWave, "two lanes a dim");
+  __shared__ u32x4 stage[kMoveThreads / kWave][kStageBlocks][kDims * kPad];
+  __shared__ int s_page[kSlots], s_off[kSlots];  // source page (-1: none) and offset of each slot
+  __shared__ int s_block[kSlots];                // its block, numbered among those of this workgroup
+  __shared__ int s_first[kSlots + 1];            // first slot of each block
+  __shared__ int s_blocks;
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int64_t chunks = (p.max_keep + kSlots - 1) / kSlots, total = chunks * p.ns * p.hkv;
   const int pgm = (1 << p.src.pg_shift) - 1;
   for (int64_t item = blockIdx.x; item < total; item += gridDim.x) {
     const int64_t row = item / chunks;
     const int b = (int)(row / p.hkv), g = (int)(row - (int64_t)b * p.hkv);
     const int s0 = (int)(item - row * chunks) * kSlots;
-    const int n = min(keep_of(p, b).keep - s0, kSlots);  // slots of this workgroup
+    const int n = min(p.new_lens[b] - s0, kSlots);  // slots of this workgroup
     if (n <= 0) continue;  // (the same for every thread)
     __syncthreads();
-    if (tid < kSlots) {
-      const int j = tid < n ? p.kept[row * p.max_keep + s0 + tid] : 0;
-      from[tid] = tid < n ? page_of(p.src, b, j) : -1;
-      off[tid] = j & pgm;
+    if (wave == 0) {
+      const bool in = lane < n;
+      const int j = in ? p.kept[row * p.max_keep + s0 + lane] : 0;
+      const int before = __shfl_up(j, 1, kWave);
+      const uint64_t starts = __ballot(in && (lane == 0 || j / kB != before / kB));
+      if (lane < kSlots) {
+        s_page[lane] = in ? page_of(p.src, b, j) : -1;
+        s_off[lane] = j & pgm;
+        const int blk = __popcll(starts & (((uint64_t)2 << lane) - 1)) - 1;
+        s_block[lane] = blk;
+        if ((starts >> lane) & 1) s_first[blk] = lane;
+      }
+      if (lane == 0) {
+        s_blocks = __popcll(starts);
+        s_first[__popcll(starts)] = n;
+      }
     }
     __syncthreads();
-    // K: 16-byte pieces in the order of the new block, so that stores are whole runs
-    const int rb = p.dst.vb_shift - 1;  // log2 of the rows of a half block
-    for (int x = tid; x < kSlots * 16; x += kCopyThreads) {
+    const u32x4 z = {0u, 0u, 0u, 0u};
+    // K: pieces in the order of the new block, so that stores are whole runs
+    constexpr int rb = kB == 32 ? 4 : 3;  // log2 of the rows of a half block
+#pragma unroll
+    for (int y = 0; y < kSlots * 16 / kMoveThreads; ++y) {
+      const int x = tid + y * kMoveThreads;
       const int r = x & ((1 << rb) - 1), piece = (x >> rb) & 3, slab = (x >> (rb + 2)) & 3, half = (x >> (rb + 4)) & 1;
       const int i = ((x >> (rb + 5)) << (rb + 1)) + 8 * (r >> 2) + 4 * half + (r & 3);
       const int d = 32 * slab + 8 * piece;
-      const int64_t to = page_of(p.dst, b, s0 + i);
-      if (i < n && to >= 0) {
-        const u32x4 z = {0u, 0u, 0u, 0u};
-        const u32x4 v = from[i] >= 0 ? ldg128(p.src.k_pool + k_offset(p.src, from[i], p.hkv, g, off[i], d)) : z;
-        stg128(p.dst.k_pool + k_offset(p.dst, to, p.hkv, g, (s0 + i) & pgm, d), v);
-      }
+      const int to = i < n ? page_of(p.dst, b, s0 + i) : -1;
+      if (to < 0) continue;
+      const u32x4 v = s_page[i] >= 0 ? ldg128(p.src.k_pool + k_offset(p.src, s_page[i], p.hkv, g, s_off[i], d)) : z;
+      stg128(p.dst.k_pool + k_offset(p.dst, to, p.hkv, g, (s0 + i) & pgm, d), v);
     }
-    // V: eight slots of one dim a thread
-    for (int x = tid; x < kSlots * 16; x += kCopyThreads) {
-      const int i0 = 8 * (x & 3), d = x >> 2;
-      const int64_t to = page_of(p.dst, b, s0 + i0);
-      if (i0 >= n || to < 0) continue;
-      uint16_t v[8];
+    // V: lane = (dim, 16 slots)
+    const int d = wave * kDims + (lane >> 1), i0 = 16 * (lane & 1);
+    uint32_t val[8] = {};  // two slots each
+    const int blocks = s_blocks;
+    for (int b0 = 0; b0 < blocks; b0 += kStageBlocks) {
+      u32x4 ld[kStageBlocks][kLoads];
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        v[e] = i0 + e < n && from[i0 + e] >= 0 ? p.src.v_pool[v_offset(p.src, from[i0 + e], p.hkv, g, off[i0 + e], d)] : 0;
+      for (int k = 0; k < kStageBlocks; ++k) {
+        const int first = s_first[min(b0 + k, blocks - 1)];
+        const int page = s_page[first];
+        const uint16_t *src = p.src.v_pool + v_offset(p.src, max(page, 0), p.hkv, g, s_off[first] & ~(kB - 1), wave * kDims);
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l)
+          ld[k][l] = b0 + k < blocks && page >= 0 ? ldg128(src + (l * kWave + lane) * 8) : z;
+      }
+      __builtin_amdgcn_wave_barrier();  // (the picks from the blocks before are done)
+#pragma unroll
+      for (int k = 0; k < kStageBlocks; ++k)
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l) {
+          const int x = l * kWave + lane;
+          stage[wave][k][x / kRow * kPad + x % kRow] = ld[k][l];
+        }
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int blk = s_block[i0 + e] - b0;
+        const uint16_t *rowp =
+            reinterpret_cast<const uint16_t *>(&stage[wave][blk & (kStageBlocks - 1)][(lane >> 1) * kPad]);
+        const uint32_t v = rowp[s_off[i0 + e] & (kB - 1)];
+        if (blk >= 0 && blk < kStageBlocks) val[e >> 1] |= v << (16 * (e & 1));
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+    const int to = i0 < n ? page_of(p.dst, b, s0 + i0) : -1;
+    if (to >= 0) {
       uint16_t *dst = p.dst.v_pool + v_offset(p.dst, to, p.hkv, g, (s0 + i0) & pgm, d);
-      if (i0 + 8 <= n) {
-        u32x4 w;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = v[2 * j] | (uint32_t)v[2 * j + 1] << 16;
-        stg128(dst, w);
-      } else {
-        for (int e = 0; i0 + e < n; ++e) dst[e] = v[e];
+      for (int h = 0; h < 2; ++h) {
+        if (i0 + 8 * h + 8 <= n) {
+          stg128(dst + 8 * h, u32x4{val[4 * h], val[4 * h + 1], val[4 * h + 2], val[4 * h + 3]});
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (i0 + 8 * h + e < n) dst[8 * h + e] = (uint16_t)(val[4 * h + (e >> 1)] >> (16 * (e & 1)));
+        }
       }
     }
   }
@@ -215,11 +320,17 @@ __global__ __launch_bounds__(kCopyThreads) void evict_move_kernel(EvictParams p)
 }  // namespace
 
 hipError_t launch_kv_evict(const EvictParams &p, hipStream_t stream) {
-  const hipError_t e = launch_kernel(evict_select_kernel, dim3((unsigned)(p.ns * p.hkv)), dim3(kSelectThreads), stream, p);
+  const dim3 rows((unsigned)(p.ns * p.hkv)), threads(kSelectThreads);
+  // scores in registers as far as they fit
+  hipError_t e;
+  if (p.max_ctx <= 4 * kSelectThreads) e = launch_kernel(evict_select_kernel<4>, rows, threads, stream, p);
+  else if (p.max_ctx <= 16 * kSelectThreads) e = launch_kernel(evict_select_kernel<16>, rows, threads, stream, p);
+  else e = launch_kernel(evict_select_kernel<0>, rows, threads, stream, p);
   if (e != hipSuccess) return e;
   const int64_t items = (int64_t)((p.max_keep + kSlots - 1) / kSlots) * p.ns * p.hkv;
-  return launch_kernel(evict_move_kernel, dim3((unsigned)std::min<int64_t>(items, kMaxCopyGrid)), dim3(kCopyThreads),
-                       stream, p);
+  const dim3 grid((unsigned)std::min<int64_t>(items, kMaxMoveGrid)), block(kMoveThreads);
+  return p.src.vb_shift == 4 ? launch_kernel(evict_move_kernel<16>, grid, block, stream, p)
+                             : launch_kernel(evict_move_kernel<32>, grid, block, stream, p);
 }
 
 }  // namespace hswa

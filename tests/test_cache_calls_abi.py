@@ -25,7 +25,7 @@ def _full():
 
 
 def _evict(layer=None, shape=None, src=None, dst=None, scores=FAKE, stride=500, ctx=FAKE, budgets=FAKE, ns=2, maxc=500,
-           recent=0, sinks=0, kept=FAKE, kstride=100, so=None, sostride=0, lens=FAKE):
+           recent=0, sinks=0, kept=FAKE, kstride=100, so=None, sostride=0, lens=FAKE2):
     return hswa.load().hswa_kv_evict(layer or _full(), ctypes.byref(shape or _shape()),
                                      ctypes.byref(src or _cache()), ctypes.byref(dst or _cache(2, 10, FAKE2)), scores,
                                      stride, ctx, budgets, ns, maxc, recent, sinks, kept, kstride, so, sostride, lens, None)
@@ -44,7 +44,7 @@ def _evict(layer=None, shape=None, src=None, dst=None, scores=FAKE, stride=500, 
     (dict(dst=_cache(8, 10, FAKE)), INVALID), (dict(so=FAKE, sostride=100), INVALID),
     (dict(src=_cache(pages=0)), INVALID),
     (dict(scores=None), INVALID), (dict(ctx=None), INVALID), (dict(budgets=None), INVALID), (dict(kept=None), INVALID),
-    (dict(lens=None), INVALID),
+    (dict(lens=None), INVALID), (dict(lens=FAKE), INVALID), (dict(lens=FAKE, ctx=0x3000), INVALID),
 ])
 def test_kv_evict_refusals(kw, code):
     assert _evict(**kw) == code
