@@ -57,7 +57,8 @@ __device__ __forceinline__ u32x4 ldnt128(const void *p) {
 //            (the log-sum-exp then gives each key's weight to fp32), every row
 //            in partials
 //   kKept    kScored that also stores the scores (in exp2 units)
-//   kSuffix  decode_shared.hip: split spans over the keys from start[b] on, a
+//   kSuffix  decode_shared.hip: split spans over the keys from start[b] on, in a
+//            kernel of its own (two waves a SIMD, one chunk in flight each), a
 //            row with keys before that in partials
 enum DecodeMode { kDecode, kScored, kKept, kSuffix };
 constexpr bool scored(int mode) { return mode == kScored || mode == kKept; }
@@ -171,9 +172,10 @@ constexpr int kCoop = kSplit ? 1 : kWaves;  // waves that share one item
 // groups). Split spans: one wave per SIMD,
 // which leaves room for two chunks of operands in flight. kOnePage: a chunk's
 // keys lie in one page (PG >= 32), else in two (PG = 16).
-template <bool kSplit, bool kOnePage, int kCGd, int kMode = kDecode>
-__global__ __launch_bounds__(kWave * kWaves) __attribute__((amdgpu_waves_per_eu(kSplit ? 1 : (kCGd == 1 ? 3 : 2))))
-void decode_kernel(DecodeParams p) {
+// span: the wave's span (kSuffix; the other modes find it from the grid).
+template <bool kSplit, bool kOnePage, int kCGd, int kMode>
+__device__ __forceinline__ void decode_waves(const DecodeParams &p, [[maybe_unused]] int64_t span) {
+  constexpr bool kDeep = kSplit && kMode != kSuffix;  // two chunks in flight
   const PoolView &pv = p.pool;
   const int lane = threadIdx.x & (kWave - 1);
   const int wid = threadIdx.x >> 6;  // wave of the workgroup
@@ -217,6 +219,9 @@ void decode_kernel(DecodeParams p) {
     total = uni64(total) * H;
     const int64_t even = (total + p.span_waves - 1) / p.span_waves;
     per = kMode == kSuffix ? *p.suffix_per : max((int64_t)(p.split_len / kChunk), even);
+    if constexpr (kMode == kSuffix) {
+      u = span * per;
+    } else {
     // Where the least length leaves fewer spans than waves, each workgroup gets
     // one before any gets a second (four to a workgroup left half the compute
     // units idle at 1 x 16K, 64 / 8 heads: 24.7 us a step against 21.9; the
@@ -224,6 +229,7 @@ void decode_kernel(DecodeParams p) {
     // share a workgroup.
     const bool few = even < per;
     u = (few ? (int64_t)wid * gridDim.x + blockIdx.x : (int64_t)blockIdx.x * kWaves + wid) * per;
+    }
     if (u >= total) return;
     u1 = min(total, u + per);
     int64_t base = 0;
@@ -555,7 +561,7 @@ void decode_kernel(DecodeParams p) {
             }
           }
         };
-        if (kSplit && nw > 0) {
+        if (kDeep && nw > 0) {
           // Split spans (long streams of chunks): one wave per SIMD, two whole
           // chunks in flight while a third is computed. Chunk k is computed
           // while k + 1 is loaded and k + 2 is issued right after k's products;
@@ -732,6 +738,12 @@ void decode_kernel(DecodeParams p) {
       }
     }
   }
+}
+
+template <bool kSplit, bool kOnePage, int kCGd, int kMode = kDecode>
+__global__ __launch_bounds__(kWave * kWaves) __attribute__((amdgpu_waves_per_eu(kSplit ? 1 : (kCGd == 1 ? 3 : 2))))
+void decode_kernel(DecodeParams p) {
+  decode_waves<kSplit, kOnePage, kCGd, kMode>(p, 0);
 }
 
 // Log-sum-exp merge of the split partials: kRowWaves waves per (sequence,

@@ -5,22 +5,28 @@
 //
 // Attention over a split key range is merged by the log-sum-exp identity, so a
 // row is the merge of its part over the prefix and its part over the
-// sequence's own keys. Four kernels:
-//   plan    one workgroup: the keys a group shares (whole tiles of 64 that every
-//           one of its queries sees), prefix sums of the work
-//   own     the keys from there on, one sequence at a time: the split decode
-//           (decode_kernels.h), bound by reading them
-//   prefix  all queries of a group against the shared keys, tiles of 64 keys
-//           in LDS under up to 256 columns, a column being a (sequence,
-//           query, head) of one KV head: bound by the matrix products and the
-//           exponentials when the group is large, by reading the keys when
-//           it is small
+// sequence's own keys. Two kernels:
+//   work    one workgroup per compute unit, of one of two kinds:
+//           prefix: all queries of a group against the shared keys, tiles of 64
+//             keys in LDS under up to 256 columns, a column being a (sequence,
+//             query, head) of one KV head. Bound by the matrix products and the
+//             exponentials where the group is large, by reading the keys where
+//             it is small.
+//           own: the keys behind the prefix, one sequence at a time, a span of
+//             32-key chunks per wave (decode_kernels.h). Bound by reading them.
+//           The plan (plan_small) divides the compute units between the two by
+//           what each has to do, so that matrix products and reads run side by
+//           side. (As kernels one after the other, 32 sequences of 100 - 1500
+//           own keys over 8192 shared ones took 23 + 26 us, 41 so.)
 //   merge   the partials of each row
-// The prefix kernel cuts the key tiles of all (group, KV head, 256 columns), in
-// that order, into equal spans, one per workgroup, each on a compute unit. Its
-// two phases (matrix products, softmax with the staging of tiles) alternate
-// between two groups of four waves, one wave of each on a SIMD, as in prefill.hip.
-// Every shared tile is whole and seen by every query, so it needs no masks.
+// Every workgroup finds the plan by itself, in one wave: a kernel for it
+// took 9 us. Batches of more than 64 sequences or 63 groups have that kernel
+// (shared_plan_kernel).
+// The key tiles of all (group, KV head, 256 columns), in that order, are cut into
+// equal spans, one per prefix workgroup. Its two phases (matrix products, softmax
+// with the staging of tiles) alternate between two groups of four waves, one
+// wave of each on a SIMD, as in prefill.hip. Every shared tile is whole and seen
+// by every query, so it needs no masks.
 #include <algorithm>
 #include <type_traits>
 
@@ -45,6 +51,11 @@ constexpr float kLaneSumLimit = 4096.f;  // a lane's share of a row sum above wh
 constexpr int kMinSpan = 4;         // least key tiles of a span
 constexpr int kMinOwn = 4;          // least chunks of a span of the own keys
 constexpr int kXcds = 8;
+constexpr int kWorkWaves = kThreads / kWave;
+// What a key tile under 128 and under 256 columns and a chunk of own keys take a
+// compute unit, in units of 0.1 us (measured with all of them at work): by these
+// the compute units are divided.
+constexpr int kCostHalf = 13, kCostFull = 22, kCostOwn = 4;
 
 __device__ __forceinline__ int64_t max64(int64_t a, int64_t b) { return a > b ? a : b; }
 
@@ -68,6 +79,116 @@ __device__ __forceinline__ int64_t block_scan(int64_t x, int64_t (&part)[kPlanWa
   return x;
 }
 
+// The division of the compute units and the spans of both kinds of work: `units`
+// key tiles worth `cost`, `chunks` chunks of own keys (of every KV head), at most
+// `longest` of one sequence.
+__device__ __forceinline__ SharedHead divide_work(const DecodeParams &d, int64_t units, int64_t cost, int64_t chunks,
+                                                  int64_t longest) {
+  SharedHead h;
+  h.units = units;
+  const float pre = (float)cost, own = (float)(chunks * kCostOwn);
+  int n = 0;  // prefix workgroups, as many on every XCD
+  if (units > 0) {
+    n = kXcds * (int)((kSharedSpans / kXcds) * pre / (pre + own) + 0.5f);
+    n = min(max(n, kXcds), kSharedSpans - kXcds);
+    if (chunks == 0) n = kSharedSpans;
+  }
+  h.prefix_groups = n;
+  h.per = n > 0 ? max64(kMinSpan, (units + n - 1) / n) : 1;
+  // spans of the own keys: at most max_splits pieces of a sequence's
+  const int waves = max(kSharedSpans - n, 1) * kWorkWaves;
+  h.own_per = max64(max64(kMinOwn, (chunks + waves - 1) / waves), (longest + d.max_splits - 2) / (d.max_splits - 1));
+  return h;
+}
+
+__device__ __forceinline__ int64_t cols_cost(int cols) {  // of a key tile under all columns of a group
+  const int full = cols / kTileCols, rest = cols - full * kTileCols;
+  return full * kCostFull + (rest == 0 ? 0 : rest <= kTileCols / 2 ? kCostHalf : kCostFull);
+}
+// The keys that a group shares, in tiles: every query of its sequences sees them
+// (`least`: the shortest context, `count` sequences with one).
+__device__ __forceinline__ int shared_tiles(const SharedParams &p, int shared, int least, int count) {
+  const int n = min(min(shared, p.max_shared), min(least, p.d.max_ctx) - p.d.nq + 1);
+  return count >= 2 && n > 0 ? n / kKT : 0;
+}
+
+// The plan of a batch of up to 64 sequences and 63 groups, by one wave: lane l
+// holds sequence l and group l. Every workgroup writes it (the same values) and
+// reads what it wrote.
+__device__ __forceinline__ void plan_small(const SharedParams &p) {
+  const DecodeParams &d = p.d;
+  const int lane = threadIdx.x & (kWave - 1);
+  const int ctx = lane < d.ns ? min(d.ctx_lens[lane], d.max_ctx) : 0;
+  // offsets that are out of range or decrease make empty groups, never overlapping ones
+  int cut = lane <= p.ng ? min(max(p.cu_groups[lane], 0), d.ns) : 0;
+  const int shared = lane < p.ng ? p.shared_lens[lane] : 0;
+#pragma unroll
+  for (int off = 1; off < kWave; off <<= 1) {
+    const int t = __shfl_up(cut, off, kWave);
+    if (lane >= off) cut = max(cut, t);
+  }
+  const int end = __shfl(cut, min(lane + 1, kWave - 1), kWave);  // of group `lane` (lane < ng)
+  const int all = __builtin_amdgcn_readlane(cut, p.ng);
+  int grp = 0;  // of sequence `lane`: the last group that starts at or before it
+  int hi = p.ng;
+#pragma unroll
+  for (int step = 0; step < 6; ++step) {  // (the same steps in every lane: the exchange needs them all)
+    const int mid = (grp + hi) >> 1;
+    const int c = __shfl(cut, mid, kWave);
+    const bool open = hi - grp > 1;
+    const int next = open && c <= lane ? mid : grp;
+    hi = open && c > lane ? mid : hi;
+    grp = next;
+  }
+  const bool member = lane >= __builtin_amdgcn_readlane(cut, 0) && lane < all;
+  grp = member ? grp : -1;
+  // the shortest context of each group, in its last sequence's lane
+  int least = ctx >= 1 ? ctx : INT32_MAX;
+#pragma unroll
+  for (int off = 1; off < kWave; off <<= 1) {
+    const int t = __shfl_up(least, off, kWave), tg = __shfl_up(grp, off, kWave);
+    if (lane >= off && tg == grp) least = min(least, t);
+  }
+  const uint64_t live = __ballot(ctx >= 1);
+  const uint64_t upto = end >= 64 ? ~0ull : ((uint64_t)1 << end) - 1;
+  const bool group = lane < p.ng && cut < end;
+  const uint64_t mine = group ? live & upto & ~(((uint64_t)1 << cut) - 1) : 0;
+  const int low = __shfl(least, max(end - 1, 0), kWave);
+  SharedGroup g;
+  g.first = cut;
+  g.leader = mine != 0 ? __builtin_ctzll(mine) : 0;
+  g.tiles = group ? shared_tiles(p, shared, low, __popcll(mine)) : 0;
+  g.cols = g.tiles > 0 ? (end - cut) * d.nq * d.group : 0;
+  const int64_t gu = (int64_t)d.hkv * ((g.cols + kTileCols - 1) / kTileCols) * g.tiles;
+  const int64_t gr = (int64_t)d.hkv * ((g.cols + kCols - 1) / kCols * kCols);
+  const int64_t su = wave_incl_scan64(gu, lane), sr = wave_incl_scan64(gr, lane);
+  const int64_t cost = wave_incl_scan64((int64_t)d.hkv * cols_cost(g.cols) * g.tiles, lane);
+  const int tiles = __shfl(g.tiles, max(grp, 0), kWave);
+  const int start = member && ctx >= 1 ? tiles * kKT : 0;
+  const int nch = ctx >= 1 ? (ctx - start + kChunk - 1) / kChunk : 0;
+  const int64_t sc = wave_incl_scan64(nch, lane);
+  int longest = nch;
+#pragma unroll
+  for (int off = 1; off < kWave; off <<= 1) longest = max(longest, __shfl_xor(longest, off, kWave));
+  const int H = d.hkv * ((d.nq * d.group + d.item_cols - 1) / d.item_cols);
+  const SharedHead h = divide_work(d, uni64(__shfl(su, kWave - 1, kWave)), uni64(__shfl(cost, kWave - 1, kWave)),
+                                   uni64(__shfl(sc, kWave - 1, kWave)) * H, longest);
+  if (lane < p.ng) {
+    p.groups[lane] = g;
+    p.group_units[lane] = su - gu;
+    p.group_rows[lane] = sr - gr;
+  }
+  if (lane < d.ns) {
+    p.start[lane] = start;
+    p.group_of[lane] = tiles > 0 ? grp : -1;
+    p.own_units[lane] = (sc - nch) * H;
+  }
+  if (lane == 0) {
+    p.group_units[p.ng] = h.units;
+    *p.head = h;
+  }
+}
+
 __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(SharedParams p) {
   __shared__ int64_t part[kPlanWaves];
   __shared__ int32_t cut[kPlanThreads + 1];  // first sequences of the groups at hand, made non-decreasing
@@ -79,7 +200,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(SharedParams 
     p.start[b] = 0;
     p.group_of[b] = -1;
   }
-  int64_t units = 0, rows = 0;  // before the groups at hand
+  int64_t units = 0, rows = 0, cost = 0;  // before the groups at hand
   int carry = 0;
   for (int i0 = 0; i0 < p.ng; i0 += kPlanThreads) {
     const int n = min(kPlanThreads, p.ng - i0);
@@ -110,9 +231,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(SharedParams 
         leader = min(leader, __shfl_xor(leader, off, kGroupLanes));
         count += __shfl_xor(count, off, kGroupLanes);
       }
-      // the first query of each sequence sees the keys up to its own position
-      const int shared = min(min(p.shared_lens[i0 + i], p.max_shared), least - d.nq + 1);
-      const int tiles = count >= 2 && shared > 0 ? shared / kKT : 0;
+      const int tiles = shared_tiles(p, p.shared_lens[i0 + i], least, count);
       if (gl == 0) {
         SharedGroup g;
         g.first = first;
@@ -128,20 +247,23 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(SharedParams 
         }
     }
     __syncthreads();
-    int64_t gu = 0, gr = 0;
+    int64_t gu = 0, gr = 0, gc = 0;
     if (tid < n) {
       const SharedGroup &g = p.groups[i0 + tid];
       gu = (int64_t)d.hkv * ((g.cols + kTileCols - 1) / kTileCols) * g.tiles;
       gr = (int64_t)d.hkv * ((g.cols + kCols - 1) / kCols * kCols);
+      gc = (int64_t)d.hkv * cols_cost(g.cols) * g.tiles;
     }
-    int64_t tu, tr;
+    int64_t tu, tr, tc;
     const int64_t su = block_scan(gu, part, tu, add), sr = block_scan(gr, part, tr, add);
+    block_scan(gc, part, tc, add);
     if (tid < n) {
       p.group_units[i0 + tid] = units + su - gu;
       p.group_rows[i0 + tid] = rows + sr - gr;
     }
     units += tu;
     rows += tr;
+    cost += tc;
   }
   // the own keys, in chunks
   __syncthreads();
@@ -158,11 +280,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(SharedParams 
   }
   if (tid == 0) {
     p.group_units[p.ng] = units;
-    p.head->units = units;
-    p.head->per = max64(kMinSpan, (units + kSharedSpans - 1) / kSharedSpans);
-    // spans of the own keys: at most max_splits pieces of a sequence's
-    const int64_t even = (chunks * H + d.span_waves - 1) / d.span_waves;
-    p.head->own_per = max64(max64(kMinOwn, even), (longest + d.max_splits - 2) / (d.max_splits - 1));
+    *p.head = divide_work(d, units, cost, chunks * H, longest);
   }
 }
 
@@ -462,15 +580,29 @@ __device__ __forceinline__ void prefix_tiles(const SharedParams &p, TileBufs &bu
   }
 }
 
-template <int kPage>
-__global__ __launch_bounds__(kThreads) void shared_prefix_kernel(SharedParams p) {
+// kCGd: 16-column groups of a wave of the own keys.
+template <int kPage, int kCGd>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void shared_work_kernel(SharedParams p) {
   __shared__ TileBufs bufs;
-  // workgroup ids go to the XCDs round-robin: an XCD gets consecutive spans,
-  // which read the same keys for other columns, or neighbouring ones
-  const int span = (int)(blockIdx.x % kXcds) * (kSharedSpans / kXcds) + (int)(blockIdx.x / kXcds);
-  const int64_t per = p.head->per;
+  const int wave = uni((int)(threadIdx.x / kWave));
+  if (p.small) {
+    if (wave == 0) plan_small(p);
+    __syncthreads();
+  }
+  // Workgroup ids go to the XCDs round-robin. An XCD gets as many of each kind
+  // as the others, and of the spans of key tiles consecutive ones, which read
+  // the same keys for other columns, or neighbouring ones.
+  const int xcd = (int)(blockIdx.x % kXcds), local = (int)(blockIdx.x / kXcds);
+  const int each = uni(p.head->prefix_groups) / kXcds;
+  if (local >= each) {
+    const int64_t first = (int64_t)xcd * (kSharedSpans / kXcds - each) + (local - each);
+    decode_waves<true, (kPage > 16), kCGd, kSuffix>(p.d, first * kWorkWaves + wave);
+    return;
+  }
+  const int span = xcd * each + local;
+  const int64_t per = uni64(p.head->per), units = uni64(p.head->units);
   int64_t u = span * per;
-  const int64_t u1 = u + per < p.head->units ? u + per : p.head->units;
+  const int64_t u1 = u + per < units ? u + per : units;
   if (u >= u1) return;
   int gi = 0;  // the group holding unit u: the last one that starts at or before it
   for (int hi = p.ng; hi - gi > 1;) {
@@ -480,7 +612,8 @@ __global__ __launch_bounds__(kThreads) void shared_prefix_kernel(SharedParams p)
   }
   for (;;) {
     while (u >= p.group_units[gi + 1]) ++gi;
-    const SharedGroup grp = p.groups[gi];
+    SharedGroup grp = p.groups[gi];
+    grp = SharedGroup{uni(grp.first), uni(grp.leader), uni(grp.tiles), uni(grp.cols)};
     const int ntc = (grp.cols + kTileCols - 1) / kTileCols;
     const int64_t rem = u - p.group_units[gi];
     const int seg = (int)(rem / grp.tiles), j0 = (int)(rem - (int64_t)seg * grp.tiles);
@@ -497,12 +630,18 @@ __global__ __launch_bounds__(kThreads) void shared_prefix_kernel(SharedParams p)
   }
 }
 
-// Merge of a row's pieces, those of the prefix and then its own: a wave per row,
-// the two half-waves take even and odd pieces, four output dims a lane.
+// Merge of a row's pieces, those of the prefix and then its own: kRowWaves waves
+// per row (see kWideMergeRows), each taking every kRowWaves-th 16 pieces; the two
+// half-waves take even and odd ones, four output dims a lane.
+template <int kRowWaves>
 __global__ __launch_bounds__(kMergeThreads) void shared_merge_kernel(SharedParams p) {
   const DecodeParams &d = p.d;
   const int lane = threadIdx.x & (kWave - 1);
-  const int64_t idx = (int64_t)blockIdx.x * (kMergeThreads / kWave) + uni((int)(threadIdx.x / kWave));
+  constexpr int kMergeWaves = kMergeThreads / kWave;
+  static_assert(kRowWaves == 1 || kRowWaves == kMergeWaves, "a row has one wave or its workgroup");
+  const int wid = uni((int)(threadIdx.x / kWave));
+  const int rw = kRowWaves == 1 ? 0 : wid;  // wave of the row
+  const int64_t idx = (int64_t)blockIdx.x * (kMergeWaves / kRowWaves) + (kRowWaves == 1 ? wid : 0);
   if (idx >= (int64_t)d.ns * d.nq * d.hq) return;
   const int b = (int)(idx / ((int64_t)d.nq * d.hq));
   const int half = lane >> 5, d4 = (lane & 31) * 4;
@@ -559,7 +698,7 @@ __global__ __launch_bounds__(kMergeThreads) void shared_merge_kernel(SharedParam
     const int s = s0 + lane;
     const float w = s < n ? fast_exp2(lse_of(s) - mx) : 0.f;
     const int m = min(kWave, n - s0);
-    for (int k0 = 0; k0 < m; k0 += 16) {
+    for (int k0 = 16 * rw; k0 < m; k0 += 16 * kRowWaves) {
       f32x4 v[8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
@@ -581,6 +720,21 @@ __global__ __launch_bounds__(kMergeThreads) void shared_merge_kernel(SharedParam
   wsum = sum_xor32(wsum);
 #pragma unroll
   for (int i = 0; i < 4; ++i) o[i] = sum_xor32(o[i]);
+  if constexpr (kRowWaves > 1) {
+    __shared__ f32x4 s_o[kRowWaves][kWave / 2];
+    __shared__ float s_w[kRowWaves];
+    if (half == 0) s_o[rw][lane] = o;
+    if (lane == 0) s_w[rw] = wsum;
+    __syncthreads();
+    if (rw != 0) return;
+    wsum = 0.f;
+    o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kRowWaves; ++w) {
+      wsum += s_w[w];
+      o += s_o[w][lane & 31];
+    }
+  }
   const float inv = 1.f / wsum;
   if (half == 0) {
     u32x2 w2;
@@ -591,36 +745,33 @@ __global__ __launch_bounds__(kMergeThreads) void shared_merge_kernel(SharedParam
 }
 
 template <int kCGd>
-hipError_t launch_cg(const SharedParams &p0, hipStream_t stream) {
-  SharedParams p = p0;
-  DecodeParams &d = p.d;
-  d.item_cols = kCols * kCGd;
-  const bool one_page = d.pool.pg_shift >= 5;
-  hipError_t e = one_page ? resident_split_waves<true, kCGd, kSuffix>(d.span_waves)
-                          : resident_split_waves<false, kCGd, kSuffix>(d.span_waves);
-  if (e != hipSuccess) return e;
-  if ((e = launch_kernel(shared_plan_kernel, dim3(1), dim3(kPlanThreads), stream, p)) != hipSuccess) return e;
-  const dim3 grid((unsigned)(d.span_waves / kWaves)), block(kWave * kWaves);
-  e = one_page ? launch_kernel(decode_kernel<true, true, kCGd, kSuffix>, grid, block, stream, d)
-               : launch_kernel(decode_kernel<true, false, kCGd, kSuffix>, grid, block, stream, d);
-  if (e != hipSuccess) return e;
-  const dim3 spans(kSharedSpans), threads(kThreads);
-  switch (d.pool.pg_shift) {
-    case 4: e = launch_kernel(shared_prefix_kernel<16>, spans, threads, stream, p); break;
-    case 5: e = launch_kernel(shared_prefix_kernel<32>, spans, threads, stream, p); break;
-    default: e = launch_kernel(shared_prefix_kernel<64>, spans, threads, stream, p);
+hipError_t launch_work(const SharedParams &p, hipStream_t stream) {
+  const dim3 grid(kSharedSpans), threads(kThreads);
+  switch (p.d.pool.pg_shift) {
+    case 4: return launch_kernel(shared_work_kernel<16, kCGd>, grid, threads, stream, p);
+    case 5: return launch_kernel(shared_work_kernel<32, kCGd>, grid, threads, stream, p);
+    default: return launch_kernel(shared_work_kernel<64, kCGd>, grid, threads, stream, p);
   }
-  if (e != hipSuccess) return e;
-  const int64_t rows = (int64_t)d.ns * d.nq * d.hq;
-  constexpr int per_block = kMergeThreads / kWave;
-  return launch_kernel(shared_merge_kernel, dim3((unsigned)((rows + per_block - 1) / per_block)), dim3(kMergeThreads),
-                       stream, p);
 }
 
 }  // namespace
 
-hipError_t launch_decode_shared(const SharedParams &p, hipStream_t stream) {
-  return p.d.nq * p.d.group > kCols ? launch_cg<2>(p, stream) : launch_cg<1>(p, stream);
+hipError_t launch_decode_shared(const SharedParams &p0, hipStream_t stream) {
+  SharedParams p = p0;
+  DecodeParams &d = p.d;
+  const bool wide_item = d.nq * d.group > kCols;
+  d.item_cols = wide_item ? 2 * kCols : kCols;
+  p.small = d.ns <= kWave && p.ng < kWave;
+  hipError_t e = p.small ? hipSuccess : launch_kernel(shared_plan_kernel, dim3(1), dim3(kPlanThreads), stream, p);
+  if (e != hipSuccess) return e;
+  e = wide_item ? launch_work<2>(p, stream) : launch_work<1>(p, stream);
+  if (e != hipSuccess) return e;
+  const int64_t rows = (int64_t)d.ns * d.nq * d.hq;
+  constexpr int per_block = kMergeThreads / kWave;
+  if (rows <= kWideMergeRows)
+    return launch_kernel(shared_merge_kernel<per_block>, dim3((unsigned)rows), dim3(kMergeThreads), stream, p);
+  return launch_kernel(shared_merge_kernel<1>, dim3((unsigned)((rows + per_block - 1) / per_block)),
+                       dim3(kMergeThreads), stream, p);
 }
 
 }  // namespace hswa

@@ -99,7 +99,7 @@ struct PrefillParams {
 // Decode over shared prefixes (decode_shared.hip). The plan, in the workspace:
 constexpr int kSharedTile = 64;    // keys of a tile of the prefix
 constexpr int kSharedCols = 256;   // (sequence, query, head) columns of a workgroup
-constexpr int kSharedSpans = 256;  // workgroups of the prefix kernel, one per compute unit
+constexpr int kSharedSpans = 256;  // workgroups of the work kernel, one per compute unit
 struct SharedGroup {
   int32_t first;   // its first sequence
   int32_t leader;  // the first with a context: the prefix is read from its row of the table
@@ -110,12 +110,14 @@ struct SharedHead {
   int64_t units;    // key tiles of all (group, KV head, kSharedCols columns)
   int64_t per;      // of them, those of a span
   int64_t own_per;  // chunks of a span of the own keys
+  int32_t prefix_groups;  // workgroups on key tiles of prefixes (a multiple of 8); the rest take own keys
 };
 struct SharedParams {
   DecodeParams d;              // the own keys; start and suffix_per point into the plan
   const int32_t *cu_groups;    // [ng + 1]
   const int32_t *shared_lens;  // [ng]
   int32_t ng, max_shared;
+  int32_t small;               // the workgroups find the plan (set at launch)
   SharedHead *head;
   SharedGroup *groups;   // [ng]
   int64_t *group_units;  // [ng + 1] units before each group
