@@ -23,7 +23,9 @@
 // took 9 us. Batches of more than 64 sequences or 63 groups have that kernel
 // (shared_plan_kernel).
 // The key tiles of all (group, KV head, 256 columns), in that order, are cut into
-// equal spans, one per prefix workgroup. Its two phases (matrix products, softmax
+// equal spans, one per prefix workgroup. Where there are few of these column
+// tiles, each is padded to a multiple of a span, so that none crosses from one to
+// the next (a second start took such a workgroup 8 of 37 us). Its two phases (matrix products, softmax
 // with the staging of tiles) alternate between two groups of four waves, one
 // wave of each on a SIMD, as in prefill.hip. Every shared tile is whole and seen
 // by every query, so it needs no masks.
@@ -52,10 +54,15 @@ constexpr int kMinSpan = 4;         // least key tiles of a span
 constexpr int kMinOwn = 4;          // least chunks of a span of the own keys
 constexpr int kXcds = 8;
 constexpr int kWorkWaves = kThreads / kWave;
-// What a key tile under 128 and under 256 columns and a chunk of own keys take a
-// compute unit, in units of 0.1 us (measured with all of them at work): by these
-// the compute units are divided.
-constexpr int kCostHalf = 13, kCostFull = 22, kCostOwn = 4;
+// What work takes, in 0.1 us (measured in place): a key tile under up to 128 and
+// under 256 columns; a workgroup's start and end on a span of them; a wave's chunk
+// of own keys with the other seven at work too (50 GB/s, what a compute unit gets
+// from HBM, whatever is in flight) and its start; all compute units' share of a
+// chunk at 5.5 TB/s; the merge of a prefix workgroup's partials.
+constexpr int kCostHalf = 11, kCostFull = 19;
+constexpr float kCostSpan = 60.f;
+constexpr float kCostOwn = 26.f, kCostOwnStart = 45.f, kCostOwnHbm = .03f, kCostMerge = .4f;
+constexpr int kAlignedGroups = 16;  // up to this many groups the plan looks for spans that end with the tiles
 
 __device__ __forceinline__ int64_t max64(int64_t a, int64_t b) { return a > b ? a : b; }
 
@@ -79,20 +86,32 @@ __device__ __forceinline__ int64_t block_scan(int64_t x, int64_t (&part)[kPlanWa
   return x;
 }
 
-// The division of the compute units and the spans of both kinds of work: `units`
-// key tiles worth `cost`, `chunks` chunks of own keys (of every KV head), at most
-// `longest` of one sequence.
+__device__ __forceinline__ int64_t cols_cost(int cols) {  // of a key tile under all columns of a group
+  const int full = cols / kTileCols, rest = cols - full * kTileCols;
+  return (int64_t)full * kCostFull + (rest == 0 ? 0 : rest <= kTileCols / 2 ? kCostHalf : kCostFull);
+}
+
+// The division of the compute units, by one wave: `units` key tiles that take
+// `cost` in all, `chunks` chunks of own keys (of every KV head), at most `longest`
+// of one sequence. Lane l tries 8 (l + 1) prefix workgroups.
 __device__ __forceinline__ SharedHead divide_work(const DecodeParams &d, int64_t units, int64_t cost, int64_t chunks,
                                                   int64_t longest) {
+  const int lane = threadIdx.x & (kWave - 1);
+  int n = 0;
+  if (units > 0) {
+    const int mine = kXcds * (min(lane, kSharedSpans / kXcds - 1) + 1);
+    const float u = (float)units, o = (float)chunks;
+    const float per = fmaxf((float)kMinSpan, ceilf(u / mine));
+    const float own_per = fmaxf((float)kMinOwn, ceilf(o / (max(kSharedSpans - mine, 1) * kWorkWaves)));
+    const float own = o == 0.f ? 0.f : mine == kSharedSpans ? FLT_MAX : kCostOwnStart + fmaxf(own_per * kCostOwn, o * kCostOwnHbm);
+    const float t = fmaxf(kCostSpan + per * ((float)cost / u), own) + mine * kCostMerge;
+    float least = t;
+#pragma unroll
+    for (int off = 1; off < kWave; off <<= 1) least = fminf(least, __shfl_xor(least, off, kWave));
+    n = kXcds * (__builtin_ctzll(__ballot(t == least)) + 1);
+  }
   SharedHead h;
   h.units = units;
-  const float pre = (float)cost, own = (float)(chunks * kCostOwn);
-  int n = 0;  // prefix workgroups, as many on every XCD
-  if (units > 0) {
-    n = kXcds * (int)((kSharedSpans / kXcds) * pre / (pre + own) + 0.5f);
-    n = min(max(n, kXcds), kSharedSpans - kXcds);
-    if (chunks == 0) n = kSharedSpans;
-  }
   h.prefix_groups = n;
   h.per = n > 0 ? max64(kMinSpan, (units + n - 1) / n) : 1;
   // spans of the own keys: at most max_splits pieces of a sequence's
@@ -101,10 +120,42 @@ __device__ __forceinline__ SharedHead divide_work(const DecodeParams &d, int64_t
   return h;
 }
 
-__device__ __forceinline__ int64_t cols_cost(int cols) {  // of a key tile under all columns of a group
-  const int full = cols / kTileCols, rest = cols - full * kTileCols;
-  return full * kCostFull + (rest == 0 ? 0 : rest <= kTileCols / 2 ? kCostHalf : kCostFull);
+// A plan's groups, by one wave that holds group l in lane l (tiles 0: none, or no
+// group): the division of the compute units, the spans, the sums before each group.
+__device__ __forceinline__ SharedHead plan_groups(const SharedParams &p, SharedGroup &g, int64_t chunks, int64_t longest,
+                                                  int64_t &units_before, int64_t &rows_before) {
+  const DecodeParams &d = p.d;
+  const int lane = threadIdx.x & (kWave - 1);
+  const auto add = [](auto a, auto b) { return a + b; };
+  const int runs = d.hkv * ((g.cols + kTileCols - 1) / kTileCols);  // column tiles of all KV heads
+  const int64_t rows = (int64_t)d.hkv * ((g.cols + kCols - 1) / kCols * kCols);
+  rows_before = wave_scan(rows, (int64_t)0, add) - rows;
+  const int64_t cost = wave_scan(d.hkv * cols_cost(g.cols) * g.tiles, (int64_t)0, add);
+  int64_t u = (int64_t)runs * g.tiles, s = wave_scan(u, (int64_t)0, add);
+  SharedHead h = divide_work(d, uni64(__shfl(s, kWave - 1, kWave)), uni64(__shfl(cost, kWave - 1, kWave)), chunks,
+                             longest);
+  g.padded = g.tiles;
+  if (h.units > 0 && p.ng <= kAlignedGroups) {
+    const int per = (int)min(h.per, (int64_t)INT32_MAX / 2) + lane;  // lane l tries this span
+    int64_t spans = 0;
+    for (int i = 0; i < p.ng; ++i) {
+      const int t = __builtin_amdgcn_readlane(g.tiles, i);
+      spans += (int64_t)__builtin_amdgcn_readlane(runs, i) * ((t + per - 1) / per);
+    }
+    const uint64_t fits = __ballot(spans <= h.prefix_groups);
+    if (fits != 0) {
+      h.per = __builtin_amdgcn_readlane(per, __builtin_ctzll(fits));
+      const int at = (int)h.per;
+      g.padded = (g.tiles + at - 1) / at * at;
+      u = (int64_t)runs * g.padded;
+      s = wave_scan(u, (int64_t)0, add);
+      h.units = uni64(__shfl(s, kWave - 1, kWave));
+    }
+  }
+  units_before = s - u;
+  return h;
 }
+
 // The keys that a group shares, in tiles: every query of its sequences sees them
 // (`least`: the shortest context, `count` sequences with one).
 __device__ __forceinline__ int shared_tiles(const SharedParams &p, int shared, int least, int count) {
@@ -113,20 +164,22 @@ __device__ __forceinline__ int shared_tiles(const SharedParams &p, int shared, i
 }
 
 // The plan of a batch of up to 64 sequences and 63 groups, by one wave: lane l
-// holds sequence l and group l. Every workgroup writes it (the same values) and
-// reads what it wrote.
-__device__ __forceinline__ void plan_small(const SharedParams &p) {
+// holds sequence l and group l. Every workgroup writes it to memory (the same
+// values), where its waves on own keys and the merge read it, and what a prefix
+// workgroup needs to LDS.
+struct SmallPlan {
+  SharedHead head;
+  SharedGroup groups[kWave];
+  int64_t units[kWave], rows[kWave];
+};
+__device__ __forceinline__ void plan_small(const SharedParams &p, SmallPlan &at) {
   const DecodeParams &d = p.d;
   const int lane = threadIdx.x & (kWave - 1);
   const int ctx = lane < d.ns ? min(d.ctx_lens[lane], d.max_ctx) : 0;
   // offsets that are out of range or decrease make empty groups, never overlapping ones
   int cut = lane <= p.ng ? min(max(p.cu_groups[lane], 0), d.ns) : 0;
   const int shared = lane < p.ng ? p.shared_lens[lane] : 0;
-#pragma unroll
-  for (int off = 1; off < kWave; off <<= 1) {
-    const int t = __shfl_up(cut, off, kWave);
-    if (lane >= off) cut = max(cut, t);
-  }
+  cut = wave_scan(cut, 0, [](int a, int b) { return max(a, b); });
   const int end = __shfl(cut, min(lane + 1, kWave - 1), kWave);  // of group `lane` (lane < ng)
   const int all = __builtin_amdgcn_readlane(cut, p.ng);
   int grp = 0;  // of sequence `lane`: the last group that starts at or before it
@@ -159,33 +212,27 @@ __device__ __forceinline__ void plan_small(const SharedParams &p) {
   g.leader = mine != 0 ? __builtin_ctzll(mine) : 0;
   g.tiles = group ? shared_tiles(p, shared, low, __popcll(mine)) : 0;
   g.cols = g.tiles > 0 ? (end - cut) * d.nq * d.group : 0;
-  const int64_t gu = (int64_t)d.hkv * ((g.cols + kTileCols - 1) / kTileCols) * g.tiles;
-  const int64_t gr = (int64_t)d.hkv * ((g.cols + kCols - 1) / kCols * kCols);
-  const int64_t su = wave_incl_scan64(gu, lane), sr = wave_incl_scan64(gr, lane);
-  const int64_t cost = wave_incl_scan64((int64_t)d.hkv * cols_cost(g.cols) * g.tiles, lane);
   const int tiles = __shfl(g.tiles, max(grp, 0), kWave);
   const int start = member && ctx >= 1 ? tiles * kKT : 0;
   const int nch = ctx >= 1 ? (ctx - start + kChunk - 1) / kChunk : 0;
-  const int64_t sc = wave_incl_scan64(nch, lane);
-  int longest = nch;
-#pragma unroll
-  for (int off = 1; off < kWave; off <<= 1) longest = max(longest, __shfl_xor(longest, off, kWave));
+  const int sc = wave_scan(nch, 0, [](int a, int b) { return a + b; });
+  const int longest = __builtin_amdgcn_readlane(wave_scan(nch, 0, [](int a, int b) { return max(a, b); }), kWave - 1);
   const int H = d.hkv * ((d.nq * d.group + d.item_cols - 1) / d.item_cols);
-  const SharedHead h = divide_work(d, uni64(__shfl(su, kWave - 1, kWave)), uni64(__shfl(cost, kWave - 1, kWave)),
-                                   uni64(__shfl(sc, kWave - 1, kWave)) * H, longest);
+  int64_t units, rows;
+  const SharedHead h = plan_groups(p, g, (int64_t)__builtin_amdgcn_readlane(sc, kWave - 1) * H, longest, units, rows);
   if (lane < p.ng) {
-    p.groups[lane] = g;
-    p.group_units[lane] = su - gu;
-    p.group_rows[lane] = sr - gr;
+    p.groups[lane] = at.groups[lane] = g;
+    p.group_units[lane] = at.units[lane] = units;
+    p.group_rows[lane] = at.rows[lane] = rows;
   }
   if (lane < d.ns) {
     p.start[lane] = start;
     p.group_of[lane] = tiles > 0 ? grp : -1;
-    p.own_units[lane] = (sc - nch) * H;
+    p.own_units[lane] = (int64_t)(sc - nch) * H;
   }
   if (lane == 0) {
-    p.group_units[p.ng] = h.units;
-    *p.head = h;
+    p.group_units[p.ng] = at.units[p.ng] = h.units;
+    *p.head = at.head = h;
   }
 }
 
@@ -236,7 +283,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(SharedParams 
         SharedGroup g;
         g.first = first;
         g.leader = leader;
-        g.tiles = tiles;
+        g.tiles = g.padded = tiles;
         g.cols = tiles > 0 ? (end - first) * d.nq * d.group : 0;
         p.groups[i0 + i] = g;
       }
@@ -252,7 +299,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(SharedParams 
       const SharedGroup &g = p.groups[i0 + tid];
       gu = (int64_t)d.hkv * ((g.cols + kTileCols - 1) / kTileCols) * g.tiles;
       gr = (int64_t)d.hkv * ((g.cols + kCols - 1) / kCols * kCols);
-      gc = (int64_t)d.hkv * cols_cost(g.cols) * g.tiles;
+      gc = d.hkv * cols_cost(g.cols) * g.tiles;
     }
     int64_t tu, tr, tc;
     const int64_t su = block_scan(gu, part, tu, add), sr = block_scan(gr, part, tr, add);
@@ -278,9 +325,24 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(SharedParams 
     chunks += total;
     longest = max64(longest, m);
   }
+  if (tid >= kWave) return;
+  SharedHead h;
+  if (p.ng < kWave) {  // few groups: as in a small plan
+    SharedGroup g{};
+    if (tid < p.ng) g = p.groups[tid];
+    int64_t before, first;
+    h = plan_groups(p, g, chunks * H, longest, before, first);
+    if (tid < p.ng) {
+      p.groups[tid] = g;
+      p.group_units[tid] = before;
+      p.group_rows[tid] = first;
+    }
+  } else {
+    h = divide_work(d, units, cost, chunks * H, longest);
+  }
   if (tid == 0) {
-    p.group_units[p.ng] = units;
-    *p.head = divide_work(d, units, cost, chunks * H, longest);
+    p.group_units[p.ng] = h.units;
+    *p.head = h;
   }
 }
 
@@ -307,6 +369,18 @@ __device__ __forceinline__ void prefix_tiles(const SharedParams &p, TileBufs &bu
   // column group cg of the wave: columns 16 (8 cg + wave) .. + 15
   const bool active = 16 * wave < ncols;  // (the first one; a wave without columns only stages)
 
+  // ---- staging: global -> registers -> LDS, in MFMA operand order ----
+  // K: the pool's 32-key blocks as they are; V^T: block (h, dt) holds, for lane
+  // r + 16 q, keys 32 h + 8 q .. + 7 of dim 16 dt + r.
+  constexpr int kPages = kKT / kPage;
+  const int vq = (tid >> 4) & 3, vdim = 16 * (tid >> 6) + (tid & 15);
+  const int last_lp = (kKT * j1 - 1) >> shift;
+  int tab_lp0 = (kKT * j0) >> shift;
+  auto load_tab = [&](int lp0) {  // lane i: the entry of logical page lp0 + i
+    const int lp = lp0 + lane;
+    return lp <= last_lp ? pv.table[(int64_t)grp.leader * pv.stride + lp] : -1;
+  };
+  int tab_page = load_tab(tab_lp0), tab_next = load_tab(tab_lp0 + kWave);
   u32x4 qf[kCG][4];
 #pragma unroll
   for (int cg = 0; cg < kCG; ++cg) {
@@ -324,18 +398,6 @@ __device__ __forceinline__ void prefix_tiles(const SharedParams &p, TileBufs &bu
     }
   }
 
-  // ---- staging: global -> registers -> LDS, in MFMA operand order ----
-  // K: the pool's 32-key blocks as they are; V^T: block (h, dt) holds, for lane
-  // r + 16 q, keys 32 h + 8 q .. + 7 of dim 16 dt + r.
-  constexpr int kPages = kKT / kPage;
-  const int vq = (tid >> 4) & 3, vdim = 16 * (tid >> 6) + (tid & 15);
-  const int last_lp = (kKT * j1 - 1) >> shift;
-  int tab_lp0 = (kKT * j0) >> shift;
-  auto load_tab = [&](int lp0) {  // lane i: the entry of logical page lp0 + i
-    const int lp = lp0 + lane;
-    return lp <= last_lp ? pv.table[(int64_t)grp.leader * pv.stride + lp] : -1;
-  };
-  int tab_page = load_tab(tab_lp0), tab_next = load_tab(tab_lp0 + kWave);
   uint32_t held = 0;  // bit 4 (j % 8) + n: the n-th 16 keys of tile j are in the pool
   u32x4 sk[kStage], sv[kStage];
   auto fetch = [&](int j, u32x4 (&k)[kStage], u32x4 (&v)[kStage]) __attribute__((always_inline)) {
@@ -584,47 +646,53 @@ __device__ __forceinline__ void prefix_tiles(const SharedParams &p, TileBufs &bu
 template <int kPage, int kCGd>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void shared_work_kernel(SharedParams p) {
   __shared__ TileBufs bufs;
+  __shared__ SmallPlan plan;
   const int wave = uni((int)(threadIdx.x / kWave));
   if (p.small) {
-    if (wave == 0) plan_small(p);
+    if (wave == 0) plan_small(p, plan);
     __syncthreads();
   }
+  const SharedHead head = p.small ? plan.head : *p.head;
   // Workgroup ids go to the XCDs round-robin. An XCD gets as many of each kind
   // as the others, and of the spans of key tiles consecutive ones, which read
   // the same keys for other columns, or neighbouring ones.
   const int xcd = (int)(blockIdx.x % kXcds), local = (int)(blockIdx.x / kXcds);
-  const int each = uni(p.head->prefix_groups) / kXcds;
+  const int each = uni(head.prefix_groups) / kXcds;
   if (local >= each) {
     const int64_t first = (int64_t)xcd * (kSharedSpans / kXcds - each) + (local - each);
     decode_waves<true, (kPage > 16), kCGd, kSuffix>(p.d, first * kWorkWaves + wave);
     return;
   }
   const int span = xcd * each + local;
-  const int64_t per = uni64(p.head->per), units = uni64(p.head->units);
+  const int64_t per = uni64(head.per), units = uni64(head.units);
   int64_t u = span * per;
   const int64_t u1 = u + per < units ? u + per : units;
   if (u >= u1) return;
+  auto units_before = [&](int i) { return uni64(p.small ? plan.units[i] : p.group_units[i]); };
   int gi = 0;  // the group holding unit u: the last one that starts at or before it
   for (int hi = p.ng; hi - gi > 1;) {
     const int mid = (gi + hi) >> 1;
-    if (p.group_units[mid] <= u) gi = mid;
+    if (units_before(mid) <= u) gi = mid;
     else hi = mid;
   }
   for (;;) {
-    while (u >= p.group_units[gi + 1]) ++gi;
-    SharedGroup grp = p.groups[gi];
-    grp = SharedGroup{uni(grp.first), uni(grp.leader), uni(grp.tiles), uni(grp.cols)};
+    while (u >= units_before(gi + 1)) ++gi;
+    SharedGroup grp = p.small ? plan.groups[gi] : p.groups[gi];
+    grp = SharedGroup{uni(grp.first), uni(grp.leader), uni(grp.tiles), uni(grp.padded), uni(grp.cols)};
     const int ntc = (grp.cols + kTileCols - 1) / kTileCols;
-    const int64_t rem = u - p.group_units[gi];
-    const int seg = (int)(rem / grp.tiles), j0 = (int)(rem - (int64_t)seg * grp.tiles);
+    const int64_t rem = u - units_before(gi);
+    const int seg = (int)(rem / grp.padded), j0 = (int)(rem - (int64_t)seg * grp.padded);
     const int g = seg / ntc, col0 = (seg - g * ntc) * kTileCols;
-    const int j1 = (int)min((int64_t)grp.tiles, j0 + (u1 - u));
+    const int left = (int)min((int64_t)(grp.padded - j0), u1 - u);  // units of this column tile in the span
+    const int j1 = min(grp.tiles, j0 + left);
     const int64_t rows = (grp.cols + kCols - 1) / kCols * kCols;
     // pieces follow each other by tile or by span: no two share a row
-    const int64_t slot = p.group_rows[gi] + g * rows + col0 + (int64_t)span * kTileCols;
-    if (grp.cols - col0 <= kTileCols / 2) prefix_tiles<1, kPage>(p, bufs, grp, g, col0, j0, j1, slot);
-    else prefix_tiles<2, kPage>(p, bufs, grp, g, col0, j0, j1, slot);
-    u += j1 - j0;
+    const int64_t slot = uni64(p.small ? plan.rows[gi] : p.group_rows[gi]) + g * rows + col0 + (int64_t)span * kTileCols;
+    if (j0 < j1) {
+      if (grp.cols - col0 <= kTileCols / 2) prefix_tiles<1, kPage>(p, bufs, grp, g, col0, j0, j1, slot);
+      else prefix_tiles<2, kPage>(p, bufs, grp, g, col0, j0, j1, slot);
+    }
+    u += left;
     if (u >= u1) return;
     __syncthreads();  // every wave has read the tile buffers
   }
@@ -664,7 +732,7 @@ __global__ __launch_bounds__(kMergeThreads) void shared_merge_kernel(SharedParam
     const SharedGroup grp = p.groups[gi];
     const int col = ((b - grp.first) * d.nq + qi) * d.group + hh;
     const int ntc = (grp.cols + kTileCols - 1) / kTileCols;
-    const int64_t seg = p.group_units[gi] + (int64_t)(g * ntc + col / kTileCols) * grp.tiles;
+    const int64_t seg = p.group_units[gi] + (int64_t)(g * ntc + col / kTileCols) * grp.padded;
     const int64_t s0 = seg / p.head->per, s1 = (seg + grp.tiles - 1) / p.head->per;
     n0 = (int)(s1 - s0) + 1;
     first = p.group_rows[gi] + (int64_t)g * ((grp.cols + kCols - 1) / kCols * kCols) + col + s0 * kTileCols;

@@ -104,10 +104,11 @@ struct SharedGroup {
   int32_t first;   // its first sequence
   int32_t leader;  // the first with a context: the prefix is read from its row of the table
   int32_t tiles;   // key tiles taken as shared (0: none)
+  int32_t padded;  // units that they take in the order of spans
   int32_t cols;    // columns of a KV head (0 without tiles)
 };
 struct SharedHead {
-  int64_t units;    // key tiles of all (group, KV head, kSharedCols columns)
+  int64_t units;    // key tiles of all (group, KV head, kSharedCols columns), padded
   int64_t per;      // of them, those of a span
   int64_t own_per;  // chunks of a span of the own keys
   int32_t prefix_groups;  // workgroups on key tiles of prefixes (a multiple of 8); the rest take own keys

@@ -136,30 +136,6 @@ struct Walk {
   int64_t next;   // where the query tile at u ends (u1 if the span ends in it)
 };
 
-// Inclusive scan over the wave's lanes with `op` (`none`: its identity) by data
-// movement inside the vector ALU; lane 63 ends up with the result of all lanes.
-template <int kCtrl, int kRows, typename T>
-__device__ __forceinline__ T lane_move(T none, T x) {
-  if constexpr (sizeof(T) == 8) {
-    const uint64_t u = __builtin_bit_cast(uint64_t, x), o = __builtin_bit_cast(uint64_t, none);
-    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp((int)o, (int)u, kCtrl, kRows, 0xf, false);
-    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp((int)(o >> 32), (int)(u >> 32), kCtrl, kRows, 0xf, false);
-    return __builtin_bit_cast(T, ((uint64_t)hi << 32) | lo);
-  } else {
-    return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, none), __builtin_bit_cast(int, x),
-                                                             kCtrl, kRows, 0xf, false));
-  }
-}
-template <typename T, typename Op>
-__device__ __forceinline__ T wave_scan(T x, T none, Op op) {
-  x = op(x, lane_move<0x111, 0xf>(none, x));  // from 1, 2, 4, 8 lanes down in a row of 16
-  x = op(x, lane_move<0x112, 0xf>(none, x));
-  x = op(x, lane_move<0x114, 0xf>(none, x));
-  x = op(x, lane_move<0x118, 0xf>(none, x));
-  x = op(x, lane_move<0x142, 0xa>(none, x));  // a row's last lane to the next row (rows 1 and 3)
-  x = op(x, lane_move<0x143, 0xc>(none, x));  // lane 31 to the upper rows
-  return x;
-}
 __device__ __forceinline__ float last_lane(float x) {
   return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), kWave - 1));
 }
