@@ -488,7 +488,8 @@ hswa_status hswa_decode_shared(hswa_layer layer, const hswa_shape *shape, const 
   p.ws_o = reinterpret_cast<float *>(ws + geo.ws_o);
   p.ws_lse = reinterpret_cast<float *>(ws + geo.ws_lse);
   p.d.start = p.start;
-  p.d.suffix_per = &p.head->own_per;
+  p.d.own_units = p.own_units;
+  p.d.own = &p.head->own;
   hipStream_t s = static_cast<hipStream_t>(stream);
   return finish_launch(hswa::launch_decode_shared(p, s), s);
 }

@@ -213,15 +213,33 @@ __device__ __forceinline__ void decode_waves(const DecodeParams &p, [[maybe_unus
   int b = 0, gy = 0;
   int64_t u = 0, u1 = 0, per = 1, pb = 0;  // span [u, u1) in units; pb: first unit of sequence b
   int nch = 0, c_lo = 0;                   // nch: chunks of sequence b
-  if constexpr (kSplit) {
+  [[maybe_unused]] int pitch = 0;          // units from one segment of a sequence to the next (nch, or whole spans)
+  if constexpr (kMode == kSuffix) {
+    const OwnSpans own = *p.own;
+    per = uni64(own.per);
+    u = span * per;
+    if (u >= uni64(own.units)) return;
+    u1 = min(uni64(own.units), u + per);
+    for (int b0 = 0;; b0 += kWave) {  // the last sequence that starts at or before u
+      const int64_t before = b0 + lane < p.ns ? p.own_units[b0 + lane] : INT64_MAX;
+      const int n = __popcll(__ballot(before <= u));
+      if (n > 0) {
+        b = b0 + n - 1;
+        pb = uni64(__shfl(before, n - 1, kWave));
+      }
+      if (n < kWave) break;
+    }
+    nch = uni(seq_chunks<kMode>(p, b));
+    pitch = uni(own.aligned) ? (int)((nch + per - 1) / per * per) : nch;
+    gy = (int)((u - pb) / pitch);
+    c_lo = (int)(u - pb - (int64_t)gy * pitch);
+    if (pitch != nch) u1 = min(u1, u + (nch - c_lo));
+  } else if constexpr (kSplit) {
     int64_t total = 0;
-    for (int s0 = 0; s0 < p.ns; s0 += kWave) total += wave_sum64(seq_chunks<kMode>(p, s0 + lane));
+    for (int s0 = 0; s0 < p.ns; s0 += kWave) total += wave_sum64(seq_chunks(p, s0 + lane));
     total = uni64(total) * H;
     const int64_t even = (total + p.span_waves - 1) / p.span_waves;
-    per = kMode == kSuffix ? *p.suffix_per : max((int64_t)(p.split_len / kChunk), even);
-    if constexpr (kMode == kSuffix) {
-      u = span * per;
-    } else {
+    per = max((int64_t)(p.split_len / kChunk), even);
     // Where the least length leaves fewer spans than waves, each workgroup gets
     // one before any gets a second (four to a workgroup left half the compute
     // units idle at 1 x 16K, 64 / 8 heads: 24.7 us a step against 21.9; the
@@ -229,12 +247,11 @@ __device__ __forceinline__ void decode_waves(const DecodeParams &p, [[maybe_unus
     // share a workgroup.
     const bool few = even < per;
     u = (few ? (int64_t)wid * gridDim.x + blockIdx.x : (int64_t)blockIdx.x * kWaves + wid) * per;
-    }
     if (u >= total) return;
     u1 = min(total, u + per);
     int64_t base = 0;
     for (int b0 = 0;; b0 += kWave) {  // the sequence holding unit u (one exists: u < total)
-      const int nchl = seq_chunks<kMode>(p, b0 + lane);
+      const int nchl = seq_chunks(p, b0 + lane);
       const int64_t incl = wave_incl_scan64((int64_t)H * nchl, lane);
       const int64_t tot = uni64(__shfl(incl, kWave - 1, kWave));
       if (u < base + tot) {
@@ -260,7 +277,7 @@ __device__ __forceinline__ void decode_waves(const DecodeParams &p, [[maybe_unus
     int c_hi = 0, piece = 0;
     bool whole = true;
     if constexpr (kSplit) {
-      const int64_t seg = pb + (int64_t)gy * nch;
+      const int64_t seg = pb + (int64_t)gy * (kMode == kSuffix ? pitch : nch);
       c_hi = (int)min((int64_t)nch, c_lo + (u1 - u));
       piece = (int)((seg + c_lo) / per - seg / per);
       whole = !scored(kMode) && c_lo == 0 && c_hi == nch;
@@ -735,6 +752,7 @@ __device__ __forceinline__ void decode_waves(const DecodeParams &p, [[maybe_unus
         pb += (int64_t)H * nch;
         do nch = uni(seq_chunks<kMode>(p, ++b));  // a scalar load
         while (nch == 0);
+        pitch = nch;  // (whole spans end with their segment)
       }
     }
   }

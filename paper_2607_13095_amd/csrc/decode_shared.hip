@@ -59,9 +59,9 @@ constexpr int kWorkWaves = kThreads / kWave;
 // of own keys with the other seven at work too (50 GB/s, what a compute unit gets
 // from HBM, whatever is in flight) and its start; all compute units' share of a
 // chunk at 5.5 TB/s; the merge of a prefix workgroup's partials.
-constexpr int kCostHalf = 11, kCostFull = 19;
-constexpr float kCostSpan = 60.f;
-constexpr float kCostOwn = 26.f, kCostOwnStart = 45.f, kCostOwnHbm = .03f, kCostMerge = .4f;
+constexpr int kCostHalf = 10, kCostFull = 19;
+constexpr float kCostSpan = 115.f;
+constexpr float kCostOwn = 26.f, kCostOwnStart = 65.f, kCostOwnHbm = .03f, kCostMerge = .4f;
 constexpr int kAlignedGroups = 16;  // up to this many groups the plan looks for spans that end with the tiles
 
 __device__ __forceinline__ int64_t max64(int64_t a, int64_t b) { return a > b ? a : b; }
@@ -116,7 +116,9 @@ __device__ __forceinline__ SharedHead divide_work(const DecodeParams &d, int64_t
   h.per = n > 0 ? max64(kMinSpan, (units + n - 1) / n) : 1;
   // spans of the own keys: at most max_splits pieces of a sequence's
   const int waves = max(kSharedSpans - n, 1) * kWorkWaves;
-  h.own_per = max64(max64(kMinOwn, (chunks + waves - 1) / waves), (longest + d.max_splits - 2) / (d.max_splits - 1));
+  h.own.units = chunks;
+  h.own.per = max64(max64(kMinOwn, (chunks + waves - 1) / waves), (longest + d.max_splits - 2) / (d.max_splits - 1));
+  h.own.aligned = 0;
   return h;
 }
 
@@ -219,7 +221,27 @@ __device__ __forceinline__ void plan_small(const SharedParams &p, SmallPlan &at)
   const int longest = __builtin_amdgcn_readlane(wave_scan(nch, 0, [](int a, int b) { return max(a, b); }), kWave - 1);
   const int H = d.hkv * ((d.nq * d.group + d.item_cols - 1) / d.item_cols);
   int64_t units, rows;
-  const SharedHead h = plan_groups(p, g, (int64_t)__builtin_amdgcn_readlane(sc, kWave - 1) * H, longest, units, rows);
+  SharedHead h = plan_groups(p, g, (int64_t)__builtin_amdgcn_readlane(sc, kWave - 1) * H, longest, units, rows);
+  // Spans of the own keys that end with their sequence and KV head: a wave that
+  // goes on with the next one starts anew there (3.5 us of about 20), which is
+  // worth a chunk more a span (2.6 us), not two.
+  int64_t before = (int64_t)(sc - nch) * H;
+  {
+    const int waves = (kSharedSpans - h.prefix_groups) * kWorkWaves / H;  // for each (KV head, column item)
+    const int segments = __popcll(__ballot(nch > 0));
+    if (waves > segments) {
+      int per = (int)h.own.per;
+      for (int tries = 0; tries < 2; ++tries, ++per) {
+        const int mine = (int)((uint32_t)(nch + per - 1) / (uint32_t)per);
+        const int all = wave_scan(mine, 0, [](int a, int b) { return a + b; });
+        if (__builtin_amdgcn_readlane(all, kWave - 1) <= waves) {
+          h.own = OwnSpans{(int64_t)__builtin_amdgcn_readlane(all, kWave - 1) * per * H, per, 1};
+          before = (int64_t)(all - mine) * per * H;
+          break;
+        }
+      }
+    }
+  }
   if (lane < p.ng) {
     p.groups[lane] = at.groups[lane] = g;
     p.group_units[lane] = at.units[lane] = units;
@@ -228,7 +250,7 @@ __device__ __forceinline__ void plan_small(const SharedParams &p, SmallPlan &at)
   if (lane < d.ns) {
     p.start[lane] = start;
     p.group_of[lane] = tiles > 0 ? grp : -1;
-    p.own_units[lane] = (int64_t)(sc - nch) * H;
+    p.own_units[lane] = before;
   }
   if (lane == 0) {
     p.group_units[p.ng] = at.units[p.ng] = h.units;
@@ -398,6 +420,15 @@ __device__ __forceinline__ void prefix_tiles(const SharedParams &p, TileBufs &bu
     }
   }
 
+  // this thread's pieces of a tile (opaque, so that the second's stays an offset of its own)
+  uint32_t koff[kStage], voff[kStage];
+#pragma unroll
+  for (int i = 0; i < kStage; ++i) {
+    const uint32_t blk = kPage == 64 ? 8192u * i : 0u;
+    koff[i] = kPage == 16 ? (uint32_t)((tid >> 4) * 128 + (tid & 7) * 16) : blk + (uint32_t)tid * 16u;
+    voff[i] = kPage == 16 ? (uint32_t)(vdim * 32 + (vq & 1) * 16) : blk + (uint32_t)(vdim * 32 + vq * 8) * 2u;
+    asm volatile("" : "+v"(koff[i]), "+v"(voff[i]));
+  }
   uint32_t held = 0;  // bit 4 (j % 8) + n: the n-th 16 keys of tile j are in the pool
   u32x4 sk[kStage], sv[kStage];
   auto fetch = [&](int j, u32x4 (&k)[kStage], u32x4 (&v)[kStage]) __attribute__((always_inline)) {
@@ -421,23 +452,25 @@ __device__ __forceinline__ void prefix_tiles(const SharedParams &p, TileBufs &bu
       const uint64_t o = ((uint64_t)((uint32_t)max(pg, 0)) * (uint32_t)d.hkv + (uint32_t)g) << (shift + kHeadDimShift + 1);
       return kPage == 64 ? o + ((uint64_t)((uint32_t)kt & ((1u << shift) - 1u)) << (kHeadDimShift + 1)) : o;
     };
+    // Bases are wave-uniform, a lane adds a fixed offset: buffer loads, without
+    // vector address arithmetic (with 16-key pages a lane chooses one of two).
+    auto load = [&](const uint16_t *pool, uint64_t o, uint32_t lane_off) __attribute__((always_inline)) {
+      const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+          const_cast<char *>(reinterpret_cast<const char *>(pool)) + o, 0, kKTileBytes, kBufferWord3);
+      return __builtin_amdgcn_raw_buffer_load_b128(rs, (int)lane_off, 0, 0);
+    };
 #pragma unroll
     for (int i = 0; i < kStage; ++i) {
-      uint64_t ko, vo;
-      uint32_t kl, vl;
       if constexpr (kPage == 16) {
         const uint64_t o0 = page_off(page[2 * i]), o1 = page_off(page[2 * i + 1]);
-        ko = tid & 8 ? o1 : o0;  // of this lane's K rows and V keys
-        vo = vq & 2 ? o1 : o0;
-        kl = (uint32_t)((tid >> 4) * 128 + (tid & 7) * 16);
-        vl = (uint32_t)(vdim * 32 + (vq & 1) * 16);
+        const uint64_t ko = tid & 8 ? o1 : o0, vo = vq & 2 ? o1 : o0;  // of this lane's K rows and V keys
+        k[i] = ldg128_global(reinterpret_cast<const char *>(pv.k_pool) + ko + koff[0]);
+        v[i] = ldg128_global(reinterpret_cast<const char *>(pv.v_pool) + vo + voff[0]);
       } else {
-        ko = vo = page_off(page[kPage == 32 ? i : 0]) + (kPage == 32 ? 0 : 8192 * i);
-        kl = (uint32_t)tid * 16u;
-        vl = (uint32_t)(vdim * 32 + vq * 8) * 2u;
+        const uint64_t o = page_off(page[kPage == 32 ? i : 0]);
+        k[i] = load(pv.k_pool, o, koff[i]);
+        v[i] = load(pv.v_pool, o, voff[i]);
       }
-      k[i] = ldg128_global(reinterpret_cast<const char *>(pv.k_pool) + ko + kl);
-      v[i] = ldg128_global(reinterpret_cast<const char *>(pv.v_pool) + vo + vl);
     }
     if (bits != 15u) {  // a page outside the pool: its keys are left out, their values zero
 #pragma unroll
@@ -742,8 +775,10 @@ __global__ __launch_bounds__(kMergeThreads) void shared_merge_kernel(SharedParam
   int n1 = 0;
   if (nch > 0) {
     const int hchunks = (d.nq * d.group + d.item_cols - 1) / d.item_cols;
-    const int64_t seg = p.own_units[b] + (int64_t)(g * hchunks + (qi * d.group + hh) / d.item_cols) * nch;
-    n1 = (int)((seg + nch - 1) / p.head->own_per - seg / p.head->own_per) + 1;
+    const OwnSpans own = p.head->own;
+    const int64_t pitch = own.aligned ? (nch + own.per - 1) / own.per * own.per : nch;
+    const int64_t seg = p.own_units[b] + (g * hchunks + (qi * d.group + hh) / d.item_cols) * pitch;
+    n1 = (int)((seg + nch - 1) / own.per - seg / own.per) + 1;
   }
   if (n0 == 0 && n1 == 1) return;  // one piece: the decode kernel wrote the row
   const int n = n0 + n1;

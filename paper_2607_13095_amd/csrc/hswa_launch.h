@@ -45,6 +45,15 @@ struct AppendParams {
   int32_t max_ctx;
 };
 
+// Suffix decode: the order of spans. Every (sequence, KV head and column item)
+// takes its chunks in units, or with `aligned` those rounded up to whole spans (a
+// span then belongs to one of them).
+struct OwnSpans {
+  int64_t units;
+  int64_t per;  // of a span
+  int32_t aligned;
+};
+
 struct DecodeParams {
   PoolView pool;
   const uint16_t *q;      // [ns][Hq][D]
@@ -70,7 +79,8 @@ struct DecodeParams {
   float *ws_s;
   int64_t max_chunks;         // 32-key chunks of max_ctx
   const int32_t *start;       // suffix decode: [ns], first key (a multiple of 32) of each sequence
-  const int64_t *suffix_per;  // and the chunks of a span
+  const int64_t *own_units;   // [ns] units before each sequence's in the order of spans
+  const OwnSpans *own;
 };
 
 // Split prefill: the query tile at the start of a span, for the merge.
@@ -110,11 +120,11 @@ struct SharedGroup {
 struct SharedHead {
   int64_t units;    // key tiles of all (group, KV head, kSharedCols columns), padded
   int64_t per;      // of them, those of a span
-  int64_t own_per;  // chunks of a span of the own keys
+  OwnSpans own;
   int32_t prefix_groups;  // workgroups on key tiles of prefixes (a multiple of 8); the rest take own keys
 };
 struct SharedParams {
-  DecodeParams d;              // the own keys; start and suffix_per point into the plan
+  DecodeParams d;              // the own keys; start, own_units and own point into the plan
   const int32_t *cu_groups;    // [ng + 1]
   const int32_t *shared_lens;  // [ng]
   int32_t ng, max_shared;
@@ -123,7 +133,7 @@ struct SharedParams {
   SharedGroup *groups;   // [ng]
   int64_t *group_units;  // [ng + 1] units before each group
   int64_t *group_rows;   // [ng] rows of partials before each group
-  int64_t *own_units;    // [ns] chunks (of every KV head) before each sequence's
+  int64_t *own_units;    // [ns] units of own keys (of every KV head) before each sequence's
   int32_t *start;        // [ns] shared keys of each sequence
   int32_t *group_of;     // [ns]
   float *ws_o;           // partial rows of the prefixes
