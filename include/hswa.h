@@ -346,10 +346,12 @@ hswa_status hswa_decode_multi(hswa_layer layer, const hswa_shape *shape, const h
  * cu_groups: device int32 [num_groups + 1], non-decreasing, within [0, ns];
  * shared_lens: device int32 [num_groups] (values above max_shared_len are
  * clamped to it, values below 64 share nothing); num_groups <= ns;
- * max_shared_len: host. Offsets out of range are clamped and decreasing ones make
- * empty groups. workspace >= hswa_decode_shared_workspace_bytes (FULL only: an
- * SWA layer reads its window, the call is hswa_decode_multi's; so it is where
- * no prefix can be shared: no group, one sequence, max_shared_len below 64).
+ * max_shared_len: host; a close bound decides best. Offsets out of range are
+ * clamped and decreasing ones make empty groups. workspace >=
+ * hswa_decode_shared_workspace_bytes (FULL only). The call is hswa_decode_multi's,
+ * bit for bit, where reading the prefixes once cannot gain: an SWA layer (it reads
+ * its window), no group, one sequence, prefixes below 64, and calls whose
+ * (ns - num_groups) * max_shared_len positions hold less than 70 MB.
  * The other arguments are as in hswa_decode_multi. */
 size_t hswa_decode_shared_workspace_bytes(const hswa_shape *shape, int32_t ns, int32_t num_queries,
                                           int32_t max_context_len, int32_t num_groups, int32_t max_shared_len);

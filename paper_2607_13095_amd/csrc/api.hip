@@ -182,10 +182,25 @@ SharedGeometry shared_geometry(const hswa_shape *sh, int32_t ns, int32_t max_ctx
   return g;
 }
 
-// Whether a call may have prefixes worth reading once: two sequences of a
-// group and a tile of shared keys.
-bool shared_fits(int32_t ns, int32_t num_groups, int32_t max_shared_len) {
-  return ns >= 2 && num_groups >= 1 && max_shared_len >= hswa::kSharedTile;
+// Whether a call goes by its prefixes: its plan, two ways of work and merge take
+// some 12 us more than a short decode, which reading less has to make up for, at
+// most (ns - num_groups) * max_shared_len positions of every KV head. us by prefix
+// and by hswa_decode_multi, 100 - 300 own tokens, with the MB saved (shared keys):
+//   64 / 8 heads   2 sequences x 8000      33 MB   26 / 22
+//                  2 x 16000               66      29 / 32
+//                  4 x 4000, 4 x 8000      49, 98  24 / 21, 27 / 30
+//                  8 x 2000, 8 x 4000      57, 115 26 / 22, 27 / 29
+//                  8 in 4 groups x 4000    66      37 / 32
+//                  32 x 1000               127     30 / 32
+//   8 / 1          8 x 16000, 8 x 32000    57, 115 23 / 20, 26 / 29
+//   16 / 16        2 x 4000, 2 x 8000      33, 66  24 / 22, 27 / 31
+//                  32 x 256                65      27 / 27
+bool shared_fits(const hswa_shape *sh, int32_t ns, int32_t num_groups, int32_t max_context_len,
+                 int32_t max_shared_len) {
+  constexpr double kLeastSaved = 70e6;
+  if (ns < 2 || num_groups < 1 || max_shared_len < hswa::kSharedTile) return false;
+  const double keys = (double)(ns - num_groups) * (max_shared_len < max_context_len ? max_shared_len : max_context_len);
+  return keys * sh->num_kv_heads * (sh->head_dim * 4) >= kLeastSaved;
 }
 
 // What every decode call tells its kernels besides the pool and the split.
@@ -442,7 +457,7 @@ size_t hswa_decode_shared_workspace_bytes(const hswa_shape *shape, int32_t ns, i
                                           int32_t max_context_len, int32_t num_groups, int32_t max_shared_len) {
   if (check_shape(shape) != HSWA_OK || ns < 1 || max_context_len < 1 || num_groups < 0 || num_groups > ns) return 0;
   if (num_queries < 1 || num_queries > kMaxQueries || max_shared_len < 0) return 0;
-  if (!shared_fits(ns, num_groups, max_shared_len))
+  if (!shared_fits(shape, ns, num_groups, max_context_len, max_shared_len))
     return hswa_decode_multi_workspace_bytes(shape, ns, num_queries, max_context_len);
   return shared_geometry(shape, ns, max_context_len, num_queries, num_groups).total_bytes;
 }
@@ -454,11 +469,10 @@ hswa_status hswa_decode_shared(hswa_layer layer, const hswa_shape *shape, const 
                                void *stream) {
   if (num_groups < 0 || max_shared_len < 0 || (ns >= 0 && num_groups > ns)) return HSWA_ERR_INVALID_ARG;
   if (num_groups > 0 && (!cu_groups || !shared_lens)) return HSWA_ERR_INVALID_ARG;
-  if (layer.kind != HSWA_LAYER_FULL || !shared_fits(ns, num_groups, max_shared_len))
+  if (layer.kind != HSWA_LAYER_FULL || check_shape(shape) != HSWA_OK || !shared_fits(shape, ns, num_groups, max_context_len, max_shared_len))
     return hswa_decode_multi(layer, shape, cache, q, context_lens, ns, num_queries, max_context_len, workspace,
                              workspace_bytes, out, stream);
   hswa_status st;
-  if ((st = check_shape(shape)) != HSWA_OK) return st;
   if (max_context_len < 1 || num_queries < 1 || num_queries > kMaxQueries) return HSWA_ERR_INVALID_ARG;
   hswa::SharedParams p{};
   if ((st = make_pool(layer, shape, cache, p.d.pool)) != HSWA_OK) return st;

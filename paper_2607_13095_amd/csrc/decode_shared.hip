@@ -65,6 +65,10 @@ constexpr float kCostOwn = 26.f, kCostOwnStart = 65.f, kCostOwnHbm = .03f, kCost
 constexpr int kAlignedGroups = 16;  // up to this many groups the plan looks for spans that end with the tiles
 
 __device__ __forceinline__ int64_t max64(int64_t a, int64_t b) { return a > b ? a : b; }
+__device__ __forceinline__ int64_t ceil_div(int64_t a, int64_t b) {  // a >= 0, b > 0
+  if (((a + b) >> 31) == 0) return ((uint32_t)a + (uint32_t)b - 1) / (uint32_t)b;  // (much shorter)
+  return (a + b - 1) / b;
+}
 
 // Inclusive scan over the workgroup of the plan with `op`; `last`: the result of all.
 template <typename Op>
@@ -105,19 +109,18 @@ __device__ __forceinline__ SharedHead divide_work(const DecodeParams &d, int64_t
     const float own_per = fmaxf((float)kMinOwn, ceilf(o / (max(kSharedSpans - mine, 1) * kWorkWaves)));
     const float own = o == 0.f ? 0.f : mine == kSharedSpans ? FLT_MAX : kCostOwnStart + fmaxf(own_per * kCostOwn, o * kCostOwnHbm);
     const float t = fmaxf(kCostSpan + per * ((float)cost / u), own) + mine * kCostMerge;
-    float least = t;
-#pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) least = fminf(least, __shfl_xor(least, off, kWave));
+    const float scan = wave_scan(t, FLT_MAX, [](float a, float b) { return fminf(a, b); });
+    const float least = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, scan), kWave - 1));
     n = kXcds * (__builtin_ctzll(__ballot(t == least)) + 1);
   }
   SharedHead h;
   h.units = units;
   h.prefix_groups = n;
-  h.per = n > 0 ? max64(kMinSpan, (units + n - 1) / n) : 1;
+  h.per = n > 0 ? max64(kMinSpan, ceil_div(units, n)) : 1;
   // spans of the own keys: at most max_splits pieces of a sequence's
   const int waves = max(kSharedSpans - n, 1) * kWorkWaves;
   h.own.units = chunks;
-  h.own.per = max64(max64(kMinOwn, (chunks + waves - 1) / waves), (longest + d.max_splits - 2) / (d.max_splits - 1));
+  h.own.per = max64(max64(kMinOwn, ceil_div(chunks, waves)), ceil_div(longest, d.max_splits - 1));
   h.own.aligned = 0;
   return h;
 }
@@ -142,13 +145,13 @@ __device__ __forceinline__ SharedHead plan_groups(const SharedParams &p, SharedG
     int64_t spans = 0;
     for (int i = 0; i < p.ng; ++i) {
       const int t = __builtin_amdgcn_readlane(g.tiles, i);
-      spans += (int64_t)__builtin_amdgcn_readlane(runs, i) * ((t + per - 1) / per);
+      spans += (int64_t)__builtin_amdgcn_readlane(runs, i) * (int)((uint32_t)(t + per - 1) / (uint32_t)per);
     }
     const uint64_t fits = __ballot(spans <= h.prefix_groups);
     if (fits != 0) {
       h.per = __builtin_amdgcn_readlane(per, __builtin_ctzll(fits));
       const int at = (int)h.per;
-      g.padded = (g.tiles + at - 1) / at * at;
+      g.padded = (int)((uint32_t)(g.tiles + at - 1) / (uint32_t)at) * at;
       u = (int64_t)runs * g.padded;
       s = wave_scan(u, (int64_t)0, add);
       h.units = uni64(__shfl(s, kWave - 1, kWave));
@@ -173,6 +176,7 @@ struct SmallPlan {
   SharedHead head;
   SharedGroup groups[kWave];
   int64_t units[kWave], rows[kWave];
+  int least[kWave];
 };
 __device__ __forceinline__ void plan_small(const SharedParams &p, SmallPlan &at) {
   const DecodeParams &d = p.d;
@@ -185,34 +189,22 @@ __device__ __forceinline__ void plan_small(const SharedParams &p, SmallPlan &at)
   const int end = __shfl(cut, min(lane + 1, kWave - 1), kWave);  // of group `lane` (lane < ng)
   const int all = __builtin_amdgcn_readlane(cut, p.ng);
   int grp = 0;  // of sequence `lane`: the last group that starts at or before it
-  int hi = p.ng;
-#pragma unroll
-  for (int step = 0; step < 6; ++step) {  // (the same steps in every lane: the exchange needs them all)
-    const int mid = (grp + hi) >> 1;
-    const int c = __shfl(cut, mid, kWave);
-    const bool open = hi - grp > 1;
-    const int next = open && c <= lane ? mid : grp;
-    hi = open && c > lane ? mid : hi;
-    grp = next;
-  }
+  for (int i = 1; i < p.ng; ++i) grp = __builtin_amdgcn_readlane(cut, i) <= lane ? i : grp;
   const bool member = lane >= __builtin_amdgcn_readlane(cut, 0) && lane < all;
   grp = member ? grp : -1;
-  // the shortest context of each group, in its last sequence's lane
-  int least = ctx >= 1 ? ctx : INT32_MAX;
-#pragma unroll
-  for (int off = 1; off < kWave; off <<= 1) {
-    const int t = __shfl_up(least, off, kWave), tg = __shfl_up(grp, off, kWave);
-    if (lane >= off && tg == grp) least = min(least, t);
-  }
+  // the shortest context of each group
+  at.least[lane] = INT32_MAX;
+  __builtin_amdgcn_wave_barrier();
+  if (member && ctx >= 1) atomicMin(&at.least[grp], ctx);
+  __builtin_amdgcn_wave_barrier();
   const uint64_t live = __ballot(ctx >= 1);
   const uint64_t upto = end >= 64 ? ~0ull : ((uint64_t)1 << end) - 1;
   const bool group = lane < p.ng && cut < end;
   const uint64_t mine = group ? live & upto & ~(((uint64_t)1 << cut) - 1) : 0;
-  const int low = __shfl(least, max(end - 1, 0), kWave);
   SharedGroup g;
   g.first = cut;
   g.leader = mine != 0 ? __builtin_ctzll(mine) : 0;
-  g.tiles = group ? shared_tiles(p, shared, low, __popcll(mine)) : 0;
+  g.tiles = group ? shared_tiles(p, shared, at.least[lane], __popcll(mine)) : 0;
   g.cols = g.tiles > 0 ? (end - cut) * d.nq * d.group : 0;
   const int tiles = __shfl(g.tiles, max(grp, 0), kWave);
   const int start = member && ctx >= 1 ? tiles * kKT : 0;

@@ -118,7 +118,7 @@ def test_decode_scored_binding_refusals():
             hswa.decode_scored(layer, shape, cache, a["q"], ctx, 32, a["si"], a["s"], q)
 
 
-def _shared(layer=None, shape=None, cache=None, q=FAKE, ctx=FAKE, ns=4, nq=1, maxc=500, cu=FAKE, sl=FAKE, ng=2, top=200,
+def _shared(layer=None, shape=None, cache=None, q=FAKE, ctx=FAKE, ns=400, nq=1, maxc=500, cu=FAKE, sl=FAKE, ng=2, top=200,
             ws=FAKE, wsb=1 << 40, out=FAKE):
     return hswa.load().hswa_decode_shared(layer or _full(), ctypes.byref(shape or _shape()),
                                           ctypes.byref(cache or _cache()), q, ctx, ns, nq, maxc, cu, sl, ng, top, ws, wsb,
@@ -130,7 +130,7 @@ def _shared(layer=None, shape=None, cache=None, q=FAKE, ctx=FAKE, ns=4, nq=1, ma
     (dict(layer=hswa._Layer(7, 1)), INVALID), (dict(layer=hswa._Layer(hswa.HSWA_LAYER_SWA, 0)), INVALID),
     (dict(shape=_shape(d=64)), UNSUPPORTED), (dict(shape=_shape(hq=63)), INVALID), (dict(shape=_shape(pg=8)), UNSUPPORTED),
     (dict(ns=-1, ng=0), INVALID), (dict(nq=0), INVALID), (dict(nq=65), INVALID), (dict(maxc=0), INVALID),
-    (dict(ng=-1), INVALID), (dict(ng=5), INVALID), (dict(top=-1), INVALID),
+    (dict(ng=-1), INVALID), (dict(ng=401), INVALID), (dict(top=-1), INVALID),
     (dict(cu=None), INVALID), (dict(sl=None), INVALID),
     (dict(cache=_cache(7)), CAPACITY), (dict(cache=_cache(pages=0)), INVALID), (dict(wsb=1000), CAPACITY),
     (dict(q=None), INVALID), (dict(ctx=None), INVALID), (dict(out=None), INVALID), (dict(ws=None), INVALID),
@@ -144,10 +144,13 @@ def test_decode_shared_refusals(kw, code):
 
 def test_decode_shared_workspace():
     sh = hswa.Shape(64, 8)
-    need = hswa.decode_shared_workspace_bytes(sh, 4, 1, 5000, 2, 1000)
-    assert need > hswa.decode_workspace_bytes(sh, 4, 5000)
-    assert hswa.decode_shared_workspace_bytes(sh, 4, 2, 5000, 0, 1000) == hswa.decode_multi_workspace_bytes(sh, 4, 2, 5000)
-    assert hswa.decode_shared_workspace_bytes(sh, 4, 1, 5000, 2, 63) == hswa.decode_workspace_bytes(sh, 4, 5000)
+    need = hswa.decode_shared_workspace_bytes(sh, 40, 1, 5000, 2, 1000)
+    assert need > hswa.decode_workspace_bytes(sh, 40, 5000)
+    # no group, prefixes below a tile, or too few positions to gain: hswa_decode_multi
+    for ns, ng, top in ((40, 0, 1000), (40, 40, 1000), (40, 2, 63), (1, 1, 5000), (4, 2, 1000), (18, 1, 1000)):
+        assert hswa.decode_shared_workspace_bytes(sh, ns, 2, 5000, ng, top) == hswa.decode_multi_workspace_bytes(
+            sh, ns, 2, 5000)
+    assert hswa.decode_shared_workspace_bytes(sh, 19, 2, 5000, 1, 1000) > hswa.decode_multi_workspace_bytes(sh, 19, 2, 5000)
     for a in ((0, 1, 100, 0, 0), (2, 0, 100, 1, 64), (2, 65, 100, 1, 64), (2, 1, 0, 1, 64), (2, 1, 100, 3, 64),
               (2, 1, 100, -1, 64), (2, 1, 100, 1, -1)):
         assert hswa.decode_shared_workspace_bytes(sh, *a) == 0

@@ -15,13 +15,14 @@ from tests.hswa_testlib import SeqHistory, append_history, assert_close, i32, ma
 pytestmark = pytest.mark.gpu
 
 D = 128
+WIDE = 150000  # a bound on the contexts under which two sequences of one KV head may gain
 
 
 class Shared:
     """A FULL layer whose rows name the same pages for the whole pages of their
     group's prefix, and pages of their own from there on."""
 
-    def __init__(self, groups, nq, hq, hkv, pg, seed, scale=None, max_ctx=None):
+    def __init__(self, groups, nq, hq, hkv, pg, seed, scale=None, max_ctx=WIDE):
         # groups: (shared tokens, [own tokens of each sequence])
         self.nq, self.hq, self.hkv, self.pg = nq, hq, hkv, pg
         self.shape = hswa.Shape(hq, hkv, D, pg, scale=scale)
@@ -45,23 +46,25 @@ class Shared:
             append_history(self.layer, self.shape, self.kv, hist, [0] * len(lens), lens)
         self.k = [np.concatenate([hist.k[i], hist.k[ng + b]]) for b, (i, _) in enumerate(own)]
         self.v = [np.concatenate([hist.v[i], hist.v[ng + b]]) for b, (i, _) in enumerate(own)]
-        self.max_ctx = max_ctx or max(max(self.ctx), 1)
+        self.max_ctx = max_ctx
         self.table = np.full((self.ns, max(1, -(-self.max_ctx // pg))), -1, np.int32)
         for b, (i, _) in enumerate(own):
             ids = list(self.kv.table_host[i][: whole[i] // pg]) + list(
                 self.kv.table_host[ng + b][: -(-lens[ng + b] // pg)])
-            self.table[b, : len(ids)] = ids
+            self.table[b, : len(ids)] = ids[: self.table.shape[1]]
         self.cu = np.concatenate([[0], np.cumsum(self.sizes)])
         self.qbits = synth.normal_bf16((self.ns, nq, hq, D), *seed, synth.TAG_QDEC)
         self.q = to_dev(self.qbits)
 
-    def run(self, cu=None, shared=None, ctx=None, table=None, max_shared=None, **kw):
+    def run(self, cu=None, shared=None, ctx=None, table=None, max_shared=WIDE, **kw):
         cu = i32(self.cu if cu is None else cu)
         shared = self.shared if shared is None else shared
         self.lens = list(self.ctx if ctx is None else ctx)
         cache = hswa.Cache(self.kv.k_pool, self.kv.v_pool, i32(self.table if table is None else table))
-        top = max(shared, default=0) if max_shared is None else max_shared
+        top = max_shared
         need = hswa.decode_shared_workspace_bytes(self.shape, self.ns, self.nq, self.max_ctx, len(shared), top)
+        plain = hswa.decode_multi_workspace_bytes(self.shape, self.ns, self.nq, self.max_ctx)
+        self.by_prefix = need != plain
         self.ws = torch.full((max(1, need),), 255, dtype=torch.uint8, device="cuda")
         self.out = torch.full_like(self.q, 7.0)
         self.args = (self.layer, self.shape, cache, self.q, i32(self.lens), self.max_ctx, cu, i32(shared), top, self.out)
@@ -69,7 +72,8 @@ class Shared:
         torch.cuda.synchronize()
         return to_f64(self.out)
 
-    def check(self, got, what, held=None):
+    def check(self, got, what, held=None, by_prefix=True):
+        assert self.by_prefix == by_prefix, what
         for b, n in enumerate(self.lens):
             n = min(n, self.max_ctx)
             ref = np.zeros((self.nq, self.hq, D))
@@ -137,27 +141,33 @@ def test_decode_shared_members_that_do_not_fit(gpu_lib):
                    dict.fromkeys(range(s.ns), 0)):
         ctx = [change.get(b, n) for b, n in enumerate(c)]
         s.check(s.run(ctx=ctx), f"contexts {change}")
-    whole = s.max_ctx
-    s.max_ctx = 650  # below some contexts: clamped
-    s.table = s.table[:, : -(-650 // 64)]
-    s.check(s.run(max_shared=700), "clamped")
-    assert whole > 650
+
+
+def test_decode_shared_clamped(gpu_lib):
+    """Contexts above max_context_len and prefixes above max_shared_len count as
+    those bounds."""
+    r = np.random.default_rng(5)
+    own = [[int(x) for x in r.integers(1, 120, n)] for n in (14, 10)]
+    s = Shared([(600, own[0]), (300, own[1])], 1, 16, 16, 64, (1513,), max_ctx=650)
+    assert max(s.ctx) > 650
+    s.check(s.run(), "contexts")
+    s = Shared([(200, [int(x) for x in r.integers(1, 30, 40)])], 1, 32, 32, 32, (1514,))
+    s.check(s.run(max_shared=128), "prefixes")
 
 
 def test_decode_shared_lengths_and_offsets_out_of_line(gpu_lib):
-    """shared_lens above max_shared_len and above the contexts' own, below 0;
-    offsets that do not cover the batch, decrease or leave it: rows stay right
+    """shared_lens above the contexts and below 0; offsets that do not cover the batch, decrease or leave it: rows stay right
     wherever the promise of equal keys holds."""
     s = Shared([(600, [20, 30, 40]), (300, [10, 20])], 1, 16, 2, 64, (1506,))
-    s.check(s.run(max_shared=128), "clamped to max_shared_len")
     s.check(s.run(shared=[600, -5]), "a negative length")
+    s.check(s.run(shared=[600, -5], cu=[3, 5, 5]), "nothing shared")
     s.check(s.run(shared=[600, 300], cu=[0, 3, 3]), "an empty group")
     s.check(s.run(shared=[600, 300], cu=[1, 3, 5]), "a sequence of no group")
     s.check(s.run(shared=[600, 300], cu=[0, 2, 2]), "the rest of no group")
     s.check(s.run(shared=[600, 300], cu=[0, 3, 1 << 30]), "past the batch")
     s.check(s.run(shared=[600, 300], cu=[-9, 3, 5]), "before the batch")
     s.check(s.run(shared=[600, 300], cu=[0, 3, 1]), "decreasing")
-    s.check(s.run(shared=[0, 300, 64, 5, 0], cu=[0, 3, 5, 2, 4, 0]), "decreasing, more of them")
+    s.check(s.run(shared=[0, 300, 64, 5], cu=[0, 3, 5, 2, 4]), "decreasing, more of them")
 
 
 def test_decode_shared_many_groups(gpu_lib):
@@ -171,15 +181,17 @@ def test_decode_shared_copied_prefix(gpu_lib):
     """Rows that hold copies of the prefix in pages of their own."""
     lens = [900, 1000, 905]
     shape = hswa.Shape(16, 2, D, 64)
-    layer, kv = make_layer("full", 0, shape, lens, (1508,))
+    layer, kv = make_layer("full", 0, shape, lens[:2] + [WIDE], (1508,))
     hist = SeqHistory(lens, 2, D, 1508)
     for b in (1, 2):
         hist.k[b][:850], hist.v[b][:850] = hist.k[0][:850], hist.v[0][:850]
     append_history(layer, shape, kv, hist, [0] * 3, lens)
     qbits = synth.normal_bf16((3, 16, D), 1508, synth.TAG_QDEC)
     out = torch.empty((3, 16, D), dtype=torch.bfloat16, device="cuda")
-    ws = torch.empty(hswa.decode_shared_workspace_bytes(shape, 3, 1, 1000, 1, 850), dtype=torch.uint8, device="cuda")
-    hswa.decode_shared(layer, shape, kv.cache, to_dev(qbits), i32(lens), 1000, i32([0, 3]), i32([850]), 850, out,
+    need = hswa.decode_shared_workspace_bytes(shape, 3, 1, WIDE, 1, WIDE)
+    assert need > hswa.decode_workspace_bytes(shape, 3, WIDE)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    hswa.decode_shared(layer, shape, kv.cache, to_dev(qbits), i32(lens), WIDE, i32([0, 3]), i32([850]), WIDE, out,
                        workspace=ws)
     torch.cuda.synchronize()
     for b, n in enumerate(lens):
@@ -201,26 +213,27 @@ def test_decode_shared_bad_pages(gpu_lib, pg):
         s.check(s.run(table=table), f"pg={pg}, pages {lost}", held=held)
 
 
-def test_decode_shared_without_sharing_is_decode_multi(gpu_lib):
-    """No group, or prefixes below a tile: the same bits as hswa_decode_multi,
-    with its workspace; an SWA layer too."""
-    s = Shared([(40, [500, 2000, 30])], 2, 16, 2, 64, (1510,))
+def test_decode_shared_without_gain_is_decode_multi(gpu_lib):
+    """No group, one sequence a group, prefixes below a tile, few positions: the
+    same bits as hswa_decode_multi, with its workspace; an SWA layer too."""
+    s = Shared([(400, [500, 2000, 30])], 2, 16, 2, 64, (1510,), max_ctx=2400)
     ws = torch.empty(max(1, hswa.decode_multi_workspace_bytes(s.shape, 3, 2, s.max_ctx)), dtype=torch.uint8,
                      device="cuda")
-    got = s.run()
-    s.check(got, "nothing shared")
+    got = s.run(max_shared=400)
+    s.check(got, "few positions", by_prefix=False)
     out = torch.empty_like(s.q)
     hswa.decode_multi(*s.args[:6], out, workspace=ws)
     torch.cuda.synchronize()
     assert np.array_equal(to_f64(out), got)
-    out.fill_(7.0)
-    hswa.decode_shared(*s.args[:6], i32([0]), i32([]), 500, out, workspace=ws)
-    torch.cuda.synchronize()
-    assert np.array_equal(to_f64(out), got)
+    for cu, sl, top in (([0], [], WIDE), ([0, 1, 2, 3], [400] * 3, WIDE), ([0, 3], [400], 63)):
+        out.fill_(7.0)
+        hswa.decode_shared(*s.args[:6], i32(cu), i32(sl), top, out, workspace=ws)
+        torch.cuda.synchronize()
+        assert np.array_equal(to_f64(out), got), cu
     layer, kv = make_layer("swa", 128, s.shape, s.ctx, (1511,))
     hist = SeqHistory(s.ctx, 2, D, 1511)
     append_history(layer, s.shape, kv, hist, [0] * 3, s.ctx)
-    hswa.decode_shared(layer, s.shape, kv.cache, s.q, i32(s.ctx), s.max_ctx, i32([0, 3]), i32([400]), 400, out)
+    hswa.decode_shared(layer, s.shape, kv.cache, s.q, i32(s.ctx), s.max_ctx, i32([0, 3]), i32([400]), WIDE, out)
     ref = torch.empty_like(out)
     hswa.decode_multi(layer, s.shape, kv.cache, s.q, i32(s.ctx), s.max_ctx, ref)
     torch.cuda.synchronize()
