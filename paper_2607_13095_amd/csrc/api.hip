@@ -129,24 +129,6 @@ DecodeGeometry decode_geometry(const hswa_shape *sh, int32_t ns, int32_t max_ctx
   return g;
 }
 
-// Scored decode: the split partials, then all scores or the rows' log-sum-exps.
-struct ScoredGeometry {
-  DecodeGeometry d;
-  bool keep;
-  int64_t max_chunks;
-  size_t total_bytes;
-};
-
-ScoredGeometry scored_geometry(const hswa_shape *sh, int32_t ns, int32_t max_ctx, int32_t nq) {
-  ScoredGeometry g{};
-  g.d = decode_geometry(sh, ns, max_ctx, nq, true);
-  const size_t rows = (size_t)ns * nq * sh->num_q_heads;
-  g.keep = nq * (sh->num_q_heads / sh->num_kv_heads) <= hswa::kKeepColumns;
-  g.max_chunks = ((int64_t)max_ctx + 31) / 32;
-  g.total_bytes = g.d.total_bytes + align_up(rows * sizeof(float) * (g.keep ? (size_t)g.max_chunks * 32 : 1), 256);
-  return g;
-}
-
 // Shared-prefix decode: the plan, the partials of the own keys, those of the
 // prefixes.
 struct SharedGeometry {
@@ -172,13 +154,38 @@ SharedGeometry shared_geometry(const hswa_shape *sh, int32_t ns, int32_t max_ctx
   g.group_of = take((size_t)ns * sizeof(int32_t));
   g.own = take(g.d.total_bytes);
   // a piece of a prefix has the rows of its columns, in 16s for a group's; each span adds at most a
-  // workgroup's columns; a group that shares has two sequences or more
+  // workgroup's columns
   const size_t cols = (size_t)ns * nq * (sh->num_q_heads / sh->num_kv_heads);
-  const size_t sharing = (size_t)(ng < ns / 2 ? ng : ns / 2);
-  const size_t rows = sh->num_kv_heads * (cols + 15 * sharing) + (size_t)hswa::kSharedSpans * hswa::kSharedCols;
+  const size_t rows = sh->num_kv_heads * (cols + 15 * (size_t)ng) + (size_t)hswa::kSharedSpans * hswa::kSharedCols;
   g.ws_o = take(rows * sh->head_dim * sizeof(float));
   g.ws_lse = take(rows * sizeof(float));
   g.total_bytes = at;
+  return g;
+}
+
+// Scored decode. Few columns: the split partials, then all scores. More: what
+// shared-prefix decode takes with each sequence a group, then the rows'
+// log-sum-exps.
+struct ScoredGeometry {
+  SharedGeometry s;
+  bool keep;
+  int64_t max_chunks;
+  size_t front, total_bytes;
+};
+
+ScoredGeometry scored_geometry(const hswa_shape *sh, int32_t ns, int32_t max_ctx, int32_t nq) {
+  ScoredGeometry g{};
+  const size_t rows = (size_t)ns * nq * sh->num_q_heads;
+  g.keep = nq * (sh->num_q_heads / sh->num_kv_heads) <= hswa::kKeepColumns;
+  g.max_chunks = ((int64_t)max_ctx + 31) / 32;
+  if (g.keep) {
+    g.s.d = decode_geometry(sh, ns, max_ctx, nq, true);
+    g.front = g.s.d.total_bytes;
+  } else {
+    g.s = shared_geometry(sh, ns, max_ctx, nq, ns);
+    g.front = g.s.total_bytes;
+  }
+  g.total_bytes = g.front + align_up(rows * sizeof(float) * (g.keep ? (size_t)g.max_chunks * 32 : 1), 256);
   return g;
 }
 
@@ -216,6 +223,30 @@ void decode_params(hswa::DecodeParams &p, const hswa_shape *shape, const void *q
   p.max_ctx = max_context_len;
   p.nq = num_queries;
   p.scale_log2 = shape->scale * 1.4426950408889634f;
+}
+
+void split_params(hswa::DecodeParams &p, const DecodeGeometry &geo, char *ws) {
+  p.split_len = geo.split_len;
+  p.max_splits = geo.max_splits;
+  p.ws_o = reinterpret_cast<float *>(ws);
+  p.ws_lse = reinterpret_cast<float *>(ws + geo.o_bytes);
+}
+
+void shared_params(hswa::SharedParams &p, const SharedGeometry &geo, int32_t num_groups, char *ws) {
+  split_params(p.d, geo.d, ws + geo.own);
+  p.ng = num_groups;
+  p.head = reinterpret_cast<hswa::SharedHead *>(ws);
+  p.groups = reinterpret_cast<hswa::SharedGroup *>(ws + geo.groups);
+  p.group_units = reinterpret_cast<int64_t *>(ws + geo.group_units);
+  p.group_rows = reinterpret_cast<int64_t *>(ws + geo.group_rows);
+  p.own_units = reinterpret_cast<int64_t *>(ws + geo.own_units);
+  p.start = reinterpret_cast<int32_t *>(ws + geo.start);
+  p.group_of = reinterpret_cast<int32_t *>(ws + geo.group_of);
+  p.ws_o = reinterpret_cast<float *>(ws + geo.ws_o);
+  p.ws_lse = reinterpret_cast<float *>(ws + geo.ws_lse);
+  p.d.start = p.start;
+  p.d.own_units = p.own_units;
+  p.d.own = &p.head->own;
 }
 
 }  // namespace
@@ -483,27 +514,10 @@ hswa_status hswa_decode_shared(hswa_layer layer, const hswa_shape *shape, const 
   const SharedGeometry geo = shared_geometry(shape, ns, max_context_len, num_queries, num_groups);
   if (workspace_bytes < geo.total_bytes) return HSWA_ERR_CAPACITY;
   decode_params(p.d, shape, q, context_lens, ns, num_queries, max_context_len, out);
-  p.d.split_len = geo.d.split_len;
-  p.d.max_splits = geo.d.max_splits;
-  char *ws = static_cast<char *>(workspace);
-  p.d.ws_o = reinterpret_cast<float *>(ws + geo.own);
-  p.d.ws_lse = reinterpret_cast<float *>(ws + geo.own + geo.d.o_bytes);
+  shared_params(p, geo, num_groups, static_cast<char *>(workspace));
   p.cu_groups = cu_groups;
   p.shared_lens = shared_lens;
-  p.ng = num_groups;
   p.max_shared = max_shared_len;
-  p.head = reinterpret_cast<hswa::SharedHead *>(ws);
-  p.groups = reinterpret_cast<hswa::SharedGroup *>(ws + geo.groups);
-  p.group_units = reinterpret_cast<int64_t *>(ws + geo.group_units);
-  p.group_rows = reinterpret_cast<int64_t *>(ws + geo.group_rows);
-  p.own_units = reinterpret_cast<int64_t *>(ws + geo.own_units);
-  p.start = reinterpret_cast<int32_t *>(ws + geo.start);
-  p.group_of = reinterpret_cast<int32_t *>(ws + geo.group_of);
-  p.ws_o = reinterpret_cast<float *>(ws + geo.ws_o);
-  p.ws_lse = reinterpret_cast<float *>(ws + geo.ws_lse);
-  p.d.start = p.start;
-  p.d.own_units = p.own_units;
-  p.d.own = &p.head->own;
   hipStream_t s = static_cast<hipStream_t>(stream);
   return finish_launch(hswa::launch_decode_shared(p, s), s);
 }
@@ -525,21 +539,26 @@ hswa_status hswa_decode_scored(hswa_layer layer, const hswa_shape *shape, const 
   if (layer.kind != HSWA_LAYER_FULL) return HSWA_ERR_UNSUPPORTED;
   if (ns < 0 || max_context_len < 1 || num_queries < 1 || num_queries > kMaxQueries) return HSWA_ERR_INVALID_ARG;
   hswa::ScoredParams p{};
-  if ((st = make_pool(layer, shape, cache, p.d.pool)) != HSWA_OK) return st;
+  if ((st = make_pool(layer, shape, cache, p.s.d.pool)) != HSWA_OK) return st;
   if ((int64_t)cache->table_stride * shape->page_size < (int64_t)max_context_len) return HSWA_ERR_CAPACITY;
   if (score_stride < max_context_len) return HSWA_ERR_CAPACITY;
   if (ns == 0) return HSWA_OK;
   if (!q || !context_lens || !out || !scores_out || !workspace) return HSWA_ERR_INVALID_ARG;
+  // (column and row numbers are 32-bit)
+  if ((int64_t)ns * num_queries * shape->num_q_heads > INT32_MAX) return HSWA_ERR_UNSUPPORTED;
   const ScoredGeometry geo = scored_geometry(shape, ns, max_context_len, num_queries);
   if (workspace_bytes < geo.total_bytes) return HSWA_ERR_CAPACITY;
-  decode_params(p.d, shape, q, context_lens, ns, num_queries, max_context_len, out);
-  p.d.split_len = geo.d.split_len;
-  p.d.max_splits = geo.d.max_splits;
+  decode_params(p.s.d, shape, q, context_lens, ns, num_queries, max_context_len, out);
   char *ws = static_cast<char *>(workspace);
-  p.d.ws_o = reinterpret_cast<float *>(ws);
-  p.d.ws_lse = reinterpret_cast<float *>(ws + geo.d.o_bytes);
-  (geo.keep ? p.d.ws_s : p.d.row_lse) = reinterpret_cast<float *>(ws + geo.d.total_bytes);
-  p.d.max_chunks = geo.max_chunks;
+  if (geo.keep) {
+    split_params(p.s.d, geo.s.d, ws);
+    p.s.d.ws_s = reinterpret_cast<float *>(ws + geo.front);
+    p.s.d.max_chunks = geo.max_chunks;
+  } else {
+    shared_params(p.s, geo.s, ns, ws);
+    p.s.max_shared = max_context_len;
+    p.s.d.row_lse = reinterpret_cast<float *>(ws + geo.front);
+  }
   p.scores_in = scores_in;
   p.scores_out = scores_out;
   p.stride = score_stride;

@@ -52,16 +52,17 @@ __device__ __forceinline__ u32x4 ldnt128(const void *p) {
 
 // What a decode kernel is for:
 //   kDecode  the decode calls: output rows
-//   kScored  decode_scored.hip: split spans whose row sums are of the
+//   kKept    decode_scored.hip: split spans whose row sums are of the
 //            probabilities in fp32, not as rounded to bf16 for the PV product
 //            (the log-sum-exp then gives each key's weight to fp32), every row
-//            in partials
-//   kKept    kScored that also stores the scores (in exp2 units)
+//            in partials, and all scores stored (in exp2 units)
 //   kSuffix  decode_shared.hip: split spans over the keys from start[b] on, in a
 //            kernel of its own (two waves a SIMD, one chunk in flight each), a
 //            row with keys before that in partials
-enum DecodeMode { kDecode, kScored, kKept, kSuffix };
-constexpr bool scored(int mode) { return mode == kScored || mode == kKept; }
+//   kSuffixScored  kSuffix with such row sums, every row in partials
+enum DecodeMode { kDecode, kKept, kSuffix, kSuffixScored };
+constexpr bool scored(int mode) { return mode == kKept || mode == kSuffixScored; }
+constexpr bool suffix(int mode) { return mode == kSuffix || mode == kSuffixScored; }
 
 constexpr int kChunk = 32;
 // Fourth word of a gfx9 buffer resource for raw accesses (32-bit data format, no
@@ -114,7 +115,7 @@ template <int kMode = kDecode>
 __device__ __forceinline__ int seq_chunks(const DecodeParams &p, int bb) {
   if (bb >= p.ns) return 0;
   int c = min(p.ctx_lens[bb], p.max_ctx);
-  if constexpr (kMode == kSuffix) c -= p.start[bb];
+  if constexpr (suffix(kMode)) c -= p.start[bb];
   return c >= 1 ? (c + kChunk - 1) / kChunk : 0;
 }
 
@@ -172,10 +173,10 @@ constexpr int kCoop = kSplit ? 1 : kWaves;  // waves that share one item
 // groups). Split spans: one wave per SIMD,
 // which leaves room for two chunks of operands in flight. kOnePage: a chunk's
 // keys lie in one page (PG >= 32), else in two (PG = 16).
-// span: the wave's span (kSuffix; the other modes find it from the grid).
+// span: the wave's span (kSuffix...; the other modes find it from the grid).
 template <bool kSplit, bool kOnePage, int kCGd, int kMode>
 __device__ __forceinline__ void decode_waves(const DecodeParams &p, [[maybe_unused]] int64_t span) {
-  constexpr bool kDeep = kSplit && kMode != kSuffix;  // two chunks in flight
+  constexpr bool kDeep = kSplit && !suffix(kMode);  // two chunks in flight
   const PoolView &pv = p.pool;
   const int lane = threadIdx.x & (kWave - 1);
   const int wid = threadIdx.x >> 6;  // wave of the workgroup
@@ -214,7 +215,7 @@ __device__ __forceinline__ void decode_waves(const DecodeParams &p, [[maybe_unus
   int64_t u = 0, u1 = 0, per = 1, pb = 0;  // span [u, u1) in units; pb: first unit of sequence b
   int nch = 0, c_lo = 0;                   // nch: chunks of sequence b
   [[maybe_unused]] int pitch = 0;          // units from one segment of a sequence to the next (nch, or whole spans)
-  if constexpr (kMode == kSuffix) {
+  if constexpr (suffix(kMode)) {
     const OwnSpans own = *p.own;
     per = uni64(own.per);
     u = span * per;
@@ -277,7 +278,7 @@ __device__ __forceinline__ void decode_waves(const DecodeParams &p, [[maybe_unus
     int c_hi = 0, piece = 0;
     bool whole = true;
     if constexpr (kSplit) {
-      const int64_t seg = pb + (int64_t)gy * (kMode == kSuffix ? pitch : nch);
+      const int64_t seg = pb + (int64_t)gy * (suffix(kMode) ? pitch : nch);
       c_hi = (int)min((int64_t)nch, c_lo + (u1 - u));
       piece = (int)((seg + c_lo) / per - seg / per);
       whole = !scored(kMode) && c_lo == 0 && c_hi == nch;
@@ -319,7 +320,7 @@ __device__ __forceinline__ void decode_waves(const DecodeParams &p, [[maybe_unus
       if (kSplit) {
         kb = c_lo * kChunk;
         ke = c_hi * kChunk - 1;
-        if constexpr (kMode == kSuffix) {
+        if constexpr (suffix(kMode)) {
           const int start = p.start[b];
           whole = whole && start == 0;
           kb += start;
@@ -768,8 +769,7 @@ void decode_kernel(DecodeParams p) {
 // query, head) row, each taking every kRowWaves-th block of 16 pieces. Lane j
 // reads the log-sum-exp of pieces j, j+64, ...; the weights are then broadcast by
 // readlane while the two half-waves accumulate even and odd pieces, four output
-// dims a lane (16-byte loads, 16 pieces in flight a step). kScored: also writes
-// the row's log-sum-exp (+infinity for a row that sees no key).
+// dims a lane (16-byte loads, 16 pieces in flight a step).
 template <int kRowWaves, int kMode = kDecode>
 __device__ __forceinline__ void merge_rows(const DecodeParams &p, int64_t block) {
   constexpr int kMergeWaves = kMergeThreads / kWave;
@@ -786,7 +786,6 @@ __device__ __forceinline__ void merge_rows(const DecodeParams &p, int64_t block)
   const u32x2 zero = {0u, 0u};
   if (ctx < 1) {
     if (half == 0) *dst = zero;
-    if (kMode == kScored && lane == 0) p.row_lse[idx] = INFINITY;
     return;
   }
   // the row's segment and the spans of the decode grid (same arithmetic as there)
@@ -817,7 +816,6 @@ __device__ __forceinline__ void merge_rows(const DecodeParams &p, int64_t block)
   mx = max_xor32(max_xor16(mx));
   if (mx == -INFINITY) {  // a query that sees no key (multi-query rows before position 0)
     if (half == 0) *dst = zero;
-    if (kMode == kScored && lane == 0) p.row_lse[idx] = INFINITY;
     return;
   }
   const float *po = p.ws_o + idx * p.max_splits * kHeadDim + d4;
@@ -867,7 +865,6 @@ __device__ __forceinline__ void merge_rows(const DecodeParams &p, int64_t block)
     }
   }
   const float inv = 1.f / wsum;
-  if (kMode == kScored && lane == 0) p.row_lse[idx] = mx + __log2f(wsum);
   if (half == 0) {
     u32x2 w2;
     w2[0] = pack_bf16x2(o[0] * inv, o[1] * inv);

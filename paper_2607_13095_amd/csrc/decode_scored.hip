@@ -8,9 +8,13 @@
 //     stores the scores in fp32, and one more kernel merges the rows and turns
 //     the scores into weights. A column costs 8 bytes a key (written and read),
 //     a key's K and V 512.
-//   more: the merge leaves the rows' log-sum-exps and a third kernel reads K a
-//     second time (256 bytes a key, whatever the columns) and forms the scores
-//     anew on the matrix cores.
+//   more: the attention is that of decode_shared.hip, every sequence a group of
+//     its own (its queries see all of its keys but the last alike), which reads
+//     the keys once for 256 columns where the split decode does for 32; its merge
+//     leaves the rows' log-sum-exps, and another kernel reads K a second time
+//     (256 bytes a key, whatever the columns) and forms the scores anew on the
+//     matrix cores. (16 queries, 32 / 8 heads, 4 x 3000 - 9000, PG 16: 41 us by
+//     the split decode, 27 so.)
 #include <algorithm>
 
 #include "decode_kernels.h"
@@ -21,7 +25,6 @@ namespace {
 constexpr int kScoreThreads = kMergeThreads;
 constexpr int kKeptKeys = 4 * kScoreThreads;  // keys of a workgroup, from kept scores
 constexpr int kMaxScoreGrid = 1 << 20;
-static_assert(kKeepColumns >= kCols, "one column group's scores are always kept");
 constexpr int kWaveChunks = 4;  // 32-key chunks a wave holds at once
 constexpr int kScoreKeys = kScoreThreads / kWave * kWaveChunks * kChunk;  // keys of a workgroup
 
@@ -41,7 +44,7 @@ __device__ __forceinline__ float row_sum16(float x) {
 // 32-key chunk lies in one page.
 template <bool kOnePage>
 __global__ __launch_bounds__(kScoreThreads) __attribute__((amdgpu_waves_per_eu(2))) void score_kernel(ScoredParams sp) {
-  const DecodeParams &p = sp.d;
+  const DecodeParams &p = sp.s.d;
   const PoolView &pv = p.pool;
   const int lane = threadIdx.x & (kWave - 1), wave = uni((int)(threadIdx.x / kWave));
   const int r = lane & 15, q = lane >> 4;
@@ -84,30 +87,41 @@ __global__ __launch_bounds__(kScoreThreads) __attribute__((amdgpu_waves_per_eu(2
     }
   }
   float w[kWaveChunks][8] = {};  // keys 8 q + i of the chunk, column r's share
-  for (int c0 = 0; c0 < ncols; c0 += kCols) {
+  // column r of a group of 16: its queries' operands and log-sum-exp, loaded a group ahead
+  struct Columns {
+    u32x4 q[4];
+    float lse;
+    int last;  // the last key it sees
+  };
+  auto load_columns = [&](int c0, Columns &x) {
     const int col = c0 + r;
     const bool valid = col < ncols;
     const int qi = valid ? col / p.group : 0;
     const int64_t row = ((int64_t)b * p.nq + qi) * p.hq + (int64_t)g * p.group + (valid ? col - qi * p.group : 0);
-    const float lse = valid ? p.row_lse[row] : INFINITY;
-    const int last = pos0 + qi;  // the last key the column sees
-    u32x4 qf[4];
+    x.lse = p.row_lse[row];
+    x.last = valid ? pos0 + qi : -1;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) qf[t] = ldg128(p.q + row * kHeadDim + 32 * t + 8 * q);
+    for (int t = 0; t < 4; ++t) x.q[t] = ldg128(p.q + row * kHeadDim + 32 * t + 8 * q);
+  };
+  Columns next;
+  load_columns(0, next);
+  for (int c0 = 0; c0 < ncols; c0 += kCols) {
+    const Columns now = next;
+    if (c0 + kCols < ncols) load_columns(c0 + kCols, next);
 #pragma unroll
     for (int c = 0; c < kWaveChunks; ++c) {
       f32x4 sa = {0.f, 0.f, 0.f, 0.f}, sb = sa;
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        sa = mfma16x16x32(ka[c][t], qf[t], sa);
-        sb = mfma16x16x32(kb[c][t], qf[t], sb);
+        sa = mfma16x16x32(ka[c][t], now.q[t], sa);
+        sb = mfma16x16x32(kb[c][t], now.q[t], sb);
       }
       const int j0 = k0 + c * kChunk + 8 * q;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float s = i < 4 ? sa[i & 3] : sb[i & 3];
-        const float e = fast_exp2(fmaf(s, p.scale_log2, -lse));
-        w[c][i] += valid && held[c] && j0 + i <= last ? e : 0.f;
+        const float e = fast_exp2(fmaf(s, p.scale_log2, -now.lse));
+        w[c][i] += held[c] && j0 + i <= now.last ? e : 0.f;
       }
     }
   }
@@ -133,7 +147,7 @@ __global__ __launch_bounds__(kScoreThreads) __attribute__((amdgpu_waves_per_eu(2
 // keys a thread.
 template <int kRowWaves>
 __global__ __launch_bounds__(kScoreThreads) void scored_finish_kernel(ScoredParams sp) {
-  const DecodeParams &p = sp.d;
+  const DecodeParams &p = sp.s.d;
   if (blockIdx.x < (unsigned)sp.merge_blocks) {
     merge_rows<kRowWaves, kKept>(p, blockIdx.x);
     return;
@@ -196,46 +210,41 @@ __global__ __launch_bounds__(kScoreThreads) void scored_finish_kernel(ScoredPara
   }
 }
 
-// The split decode, with `kMode`, and what follows it.
-template <int kCGd, int kMode>
-hipError_t launch_cg(const ScoredParams &p0, hipStream_t stream) {
+hipError_t launch_kept(const ScoredParams &p0, hipStream_t stream) {
+  constexpr int kCGd = 1;
+  static_assert(kKeepColumns <= kCGd * kCols, "one column item per KV head");
   ScoredParams sp = p0;
-  DecodeParams &p = sp.d;
+  DecodeParams &p = sp.s.d;
   p.item_cols = kCols * kCGd;
   const bool one_page = p.pool.pg_shift >= 5;
-  hipError_t e = one_page ? resident_split_waves<true, kCGd, kMode>(p.span_waves)
-                          : resident_split_waves<false, kCGd, kMode>(p.span_waves);
+  hipError_t e = one_page ? resident_split_waves<true, kCGd, kKept>(p.span_waves)
+                          : resident_split_waves<false, kCGd, kKept>(p.span_waves);
   if (e != hipSuccess) return e;
   const dim3 grid((unsigned)(p.span_waves / kWaves)), block(kWave * kWaves), threads(kScoreThreads);
-  e = one_page ? launch_kernel(decode_kernel<true, true, kCGd, kMode>, grid, block, stream, p)
-               : launch_kernel(decode_kernel<true, false, kCGd, kMode>, grid, block, stream, p);
+  e = one_page ? launch_kernel(decode_kernel<true, true, kCGd, kKept>, grid, block, stream, p)
+               : launch_kernel(decode_kernel<true, false, kCGd, kKept>, grid, block, stream, p);
   if (e != hipSuccess) return e;
   const int64_t rows = (int64_t)p.ns * p.nq * p.hq;
   constexpr int per_block = kMergeThreads / kWave;
   const bool wide = rows <= kWideMergeRows;
-  const dim3 merge((unsigned)(wide ? rows : (rows + per_block - 1) / per_block));
-  const int64_t keys = kMode == kKept ? kKeptKeys : kScoreKeys;
-  const dim3 items((unsigned)std::min<int64_t>((int64_t)p.ns * p.hkv * ((p.max_ctx + keys - 1) / keys), kMaxScoreGrid));
-  if constexpr (kMode == kKept) {
-    sp.merge_blocks = merge.x;
-    const dim3 both(merge.x + items.x);
-    return wide ? launch_kernel(scored_finish_kernel<per_block>, both, threads, stream, sp)
-                : launch_kernel(scored_finish_kernel<1>, both, threads, stream, sp);
-  } else {
-    e = wide ? launch_kernel(decode_merge_kernel<per_block, kScored>, merge, threads, stream, p)
-             : launch_kernel(decode_merge_kernel<1, kScored>, merge, threads, stream, p);
-    if (e != hipSuccess) return e;
-    return one_page ? launch_kernel(score_kernel<true>, items, threads, stream, sp)
-                    : launch_kernel(score_kernel<false>, items, threads, stream, sp);
-  }
+  sp.merge_blocks = wide ? rows : (rows + per_block - 1) / per_block;
+  const int64_t items = (int64_t)p.ns * p.hkv * ((p.max_ctx + kKeptKeys - 1) / kKeptKeys);
+  const dim3 both((unsigned)(sp.merge_blocks + std::min<int64_t>(items, kMaxScoreGrid)));
+  return wide ? launch_kernel(scored_finish_kernel<per_block>, both, threads, stream, sp)
+              : launch_kernel(scored_finish_kernel<1>, both, threads, stream, sp);
 }
 
 }  // namespace
 
 hipError_t launch_decode_scored(const ScoredParams &p, hipStream_t stream) {
-  const int columns = p.d.nq * p.d.group;
-  if (columns <= kCols) return launch_cg<1, kKept>(p, stream);
-  return columns <= kKeepColumns ? launch_cg<2, kKept>(p, stream) : launch_cg<2, kScored>(p, stream);
+  const DecodeParams &d = p.s.d;
+  if (d.nq * d.group <= kKeepColumns) return launch_kept(p, stream);
+  const hipError_t e = launch_decode_shared_scored(p.s, stream);
+  if (e != hipSuccess) return e;
+  const int64_t items = (int64_t)d.ns * d.hkv * ((d.max_ctx + kScoreKeys - 1) / kScoreKeys);
+  const dim3 grid((unsigned)std::min<int64_t>(items, kMaxScoreGrid)), threads(kScoreThreads);
+  return d.pool.pg_shift >= 5 ? launch_kernel(score_kernel<true>, grid, threads, stream, p)
+                              : launch_kernel(score_kernel<false>, grid, threads, stream, p);
 }
 
 }  // namespace hswa

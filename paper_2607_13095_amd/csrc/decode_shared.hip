@@ -165,7 +165,12 @@ __device__ __forceinline__ SharedHead plan_groups(const SharedParams &p, SharedG
 // (`least`: the shortest context, `count` sequences with one).
 __device__ __forceinline__ int shared_tiles(const SharedParams &p, int shared, int least, int count) {
   const int n = min(min(shared, p.max_shared), min(least, p.d.max_ctx) - p.d.nq + 1);
-  return count >= 2 && n > 0 ? n / kKT : 0;
+  return count >= (p.cu_groups ? 2 : 1) && n > 0 ? n / kKT : 0;
+}
+// Group i's first sequence and the length that its sequences share, as given.
+__device__ __forceinline__ int group_first(const SharedParams &p, int i) { return p.cu_groups ? p.cu_groups[i] : i; }
+__device__ __forceinline__ int group_shared(const SharedParams &p, int i) {
+  return p.cu_groups ? p.shared_lens[i] : INT32_MAX;
 }
 
 // The plan of a batch of up to 64 sequences and 63 groups, by one wave: lane l
@@ -183,8 +188,8 @@ __device__ __forceinline__ void plan_small(const SharedParams &p, SmallPlan &at)
   const int lane = threadIdx.x & (kWave - 1);
   const int ctx = lane < d.ns ? min(d.ctx_lens[lane], d.max_ctx) : 0;
   // offsets that are out of range or decrease make empty groups, never overlapping ones
-  int cut = lane <= p.ng ? min(max(p.cu_groups[lane], 0), d.ns) : 0;
-  const int shared = lane < p.ng ? p.shared_lens[lane] : 0;
+  int cut = lane <= p.ng ? min(max(group_first(p, lane), 0), d.ns) : 0;
+  const int shared = lane < p.ng ? group_shared(p, lane) : 0;
   cut = wave_scan(cut, 0, [](int a, int b) { return max(a, b); });
   const int end = __shfl(cut, min(lane + 1, kWave - 1), kWave);  // of group `lane` (lane < ng)
   const int all = __builtin_amdgcn_readlane(cut, p.ng);
@@ -266,7 +271,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(SharedParams 
   for (int i0 = 0; i0 < p.ng; i0 += kPlanThreads) {
     const int n = min(kPlanThreads, p.ng - i0);
     // offsets that are out of range or decrease make empty groups, never overlapping ones
-    auto offset = [&](int i) { return (int64_t)min(max(p.cu_groups[i0 + i], 0), d.ns); };
+    auto offset = [&](int i) { return (int64_t)min(max(group_first(p, i0 + i), 0), d.ns); };
     int64_t all;
     const int64_t c = block_scan(max64(tid < n ? offset(tid) : 0, carry), part, all, most);
     if (tid < n) cut[tid] = (int)c;
@@ -292,7 +297,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(SharedParams 
         leader = min(leader, __shfl_xor(leader, off, kGroupLanes));
         count += __shfl_xor(count, off, kGroupLanes);
       }
-      const int tiles = shared_tiles(p, p.shared_lens[i0 + i], least, count);
+      const int tiles = shared_tiles(p, group_shared(p, i0 + i), least, count);
       if (gl == 0) {
         SharedGroup g;
         g.first = first;
@@ -367,8 +372,8 @@ struct __attribute__((aligned(16))) TileBufs {
 // Key tiles [j0, j1) of a group (its leader's row of the block table) for KV
 // head g and the columns from col0 on: partial rows to slot, slot + 1, ... of
 // the workspace. kCG: 16-column groups of a wave. kPage: keys of a page, 64
-// standing for 64 and more.
-template <int kCG, int kPage>
+// standing for 64 and more. kMode: as for the own keys.
+template <int kCG, int kPage, int kMode>
 __device__ __forceinline__ void prefix_tiles(const SharedParams &p, TileBufs &bufs, const SharedGroup &grp, int g,
                                              int col0, int j0, int j1, int64_t slot) {
   unsigned char *const s_lds = bufs.b;
@@ -538,8 +543,12 @@ __device__ __forceinline__ void prefix_tiles(const SharedParams &p, TileBufs &bu
         for (int e = 0; e < 8; ++e) pr[e] = fast_exp2(fmaf(sc[h][e >> 2][cg][e & 3], c2, -mc));
 #pragma unroll
         for (int j = 0; j < 4; ++j) pf[h][cg][j] = pack_bf16x2(pr[2 * j], pr[2 * j + 1]);
+        if constexpr (scored(kMode)) {
+          ts[cg] += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
+        } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) ts[cg] = dot2_bf16_ones(pf[h][cg][j], ts[cg]);
+          for (int j = 0; j < 4; ++j) ts[cg] = dot2_bf16_ones(pf[h][cg][j], ts[cg]);
+        }
       }
     }
   };
@@ -667,8 +676,8 @@ __device__ __forceinline__ void prefix_tiles(const SharedParams &p, TileBufs &bu
   }
 }
 
-// kCGd: 16-column groups of a wave of the own keys.
-template <int kPage, int kCGd>
+// kCGd: 16-column groups of a wave of the own keys. kMode: kSuffix, kSuffixScored.
+template <int kPage, int kCGd, int kMode>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void shared_work_kernel(SharedParams p) {
   __shared__ TileBufs bufs;
   __shared__ SmallPlan plan;
@@ -685,7 +694,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   const int each = uni(head.prefix_groups) / kXcds;
   if (local >= each) {
     const int64_t first = (int64_t)xcd * (kSharedSpans / kXcds - each) + (local - each);
-    decode_waves<true, (kPage > 16), kCGd, kSuffix>(p.d, first * kWorkWaves + wave);
+    decode_waves<true, (kPage > 16), kCGd, kMode>(p.d, first * kWorkWaves + wave);
     return;
   }
   const int span = xcd * each + local;
@@ -714,8 +723,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     // pieces follow each other by tile or by span: no two share a row
     const int64_t slot = uni64(p.small ? plan.rows[gi] : p.group_rows[gi]) + g * rows + col0 + (int64_t)span * kTileCols;
     if (j0 < j1) {
-      if (grp.cols - col0 <= kTileCols / 2) prefix_tiles<1, kPage>(p, bufs, grp, g, col0, j0, j1, slot);
-      else prefix_tiles<2, kPage>(p, bufs, grp, g, col0, j0, j1, slot);
+      if (grp.cols - col0 <= kTileCols / 2) prefix_tiles<1, kPage, kMode>(p, bufs, grp, g, col0, j0, j1, slot);
+      else prefix_tiles<2, kPage, kMode>(p, bufs, grp, g, col0, j0, j1, slot);
     }
     u += left;
     if (u >= u1) return;
@@ -725,8 +734,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 
 // Merge of a row's pieces, those of the prefix and then its own: kRowWaves waves
 // per row (see kWideMergeRows), each taking every kRowWaves-th 16 pieces; the two
-// half-waves take even and odd ones, four output dims a lane.
-template <int kRowWaves>
+// half-waves take even and odd ones, four output dims a lane. kSuffixScored: also
+// writes the row's log-sum-exp (+infinity for a row that sees no key).
+template <int kRowWaves, int kMode>
 __global__ __launch_bounds__(kMergeThreads) void shared_merge_kernel(SharedParams p) {
   const DecodeParams &d = p.d;
   const int lane = threadIdx.x & (kWave - 1);
@@ -743,6 +753,7 @@ __global__ __launch_bounds__(kMergeThreads) void shared_merge_kernel(SharedParam
   const int ctx = min(d.ctx_lens[b], d.max_ctx);
   if (ctx < 1) {
     if (half == 0) *dst = zero;
+    if (scored(kMode) && lane == 0) d.row_lse[idx] = INFINITY;
     return;
   }
   const int rem = (int)(idx - (int64_t)b * d.nq * d.hq);
@@ -772,7 +783,7 @@ __global__ __launch_bounds__(kMergeThreads) void shared_merge_kernel(SharedParam
     const int64_t seg = p.own_units[b] + (g * hchunks + (qi * d.group + hh) / d.item_cols) * pitch;
     n1 = (int)((seg + nch - 1) / own.per - seg / own.per) + 1;
   }
-  if (n0 == 0 && n1 == 1) return;  // one piece: the decode kernel wrote the row
+  if (!scored(kMode) && n0 == 0 && n1 == 1) return;  // one piece: the decode kernel wrote the row
   const int n = n0 + n1;
   auto lse_of = [&](int s) {
     return s < n0 ? p.ws_lse[first + (int64_t)s * kTileCols] : d.ws_lse[idx * d.max_splits + s - n0];
@@ -784,6 +795,7 @@ __global__ __launch_bounds__(kMergeThreads) void shared_merge_kernel(SharedParam
   mx = max_xor32(max_xor16(mx));
   if (mx == -INFINITY) {  // a row that sees no key
     if (half == 0) *dst = zero;
+    if (scored(kMode) && lane == 0) d.row_lse[idx] = INFINITY;
     return;
   }
   const float *po0 = p.ws_o + first * kHeadDim + d4, *po1 = d.ws_o + (idx * d.max_splits - n0) * kHeadDim + d4;
@@ -830,6 +842,7 @@ __global__ __launch_bounds__(kMergeThreads) void shared_merge_kernel(SharedParam
       o += s_o[w][lane & 31];
     }
   }
+  if (scored(kMode) && lane == 0) d.row_lse[idx] = mx + __log2f(wsum);
   const float inv = 1.f / wsum;
   if (half == 0) {
     u32x2 w2;
@@ -839,34 +852,41 @@ __global__ __launch_bounds__(kMergeThreads) void shared_merge_kernel(SharedParam
   }
 }
 
-template <int kCGd>
+template <int kCGd, int kMode>
 hipError_t launch_work(const SharedParams &p, hipStream_t stream) {
   const dim3 grid(kSharedSpans), threads(kThreads);
   switch (p.d.pool.pg_shift) {
-    case 4: return launch_kernel(shared_work_kernel<16, kCGd>, grid, threads, stream, p);
-    case 5: return launch_kernel(shared_work_kernel<32, kCGd>, grid, threads, stream, p);
-    default: return launch_kernel(shared_work_kernel<64, kCGd>, grid, threads, stream, p);
+    case 4: return launch_kernel(shared_work_kernel<16, kCGd, kMode>, grid, threads, stream, p);
+    case 5: return launch_kernel(shared_work_kernel<32, kCGd, kMode>, grid, threads, stream, p);
+    default: return launch_kernel(shared_work_kernel<64, kCGd, kMode>, grid, threads, stream, p);
   }
+}
+
+template <int kCGd, int kMode>
+hipError_t launch_cg(const SharedParams &p0, hipStream_t stream) {
+  SharedParams p = p0;
+  DecodeParams &d = p.d;
+  d.item_cols = kCGd * kCols;
+  p.small = d.ns <= kWave && p.ng < kWave;
+  hipError_t e = p.small ? hipSuccess : launch_kernel(shared_plan_kernel, dim3(1), dim3(kPlanThreads), stream, p);
+  if (e != hipSuccess) return e;
+  if ((e = launch_work<kCGd, kMode>(p, stream)) != hipSuccess) return e;
+  const int64_t rows = (int64_t)d.ns * d.nq * d.hq;
+  constexpr int per_block = kMergeThreads / kWave;
+  if (rows <= kWideMergeRows)
+    return launch_kernel(shared_merge_kernel<per_block, kMode>, dim3((unsigned)rows), dim3(kMergeThreads), stream, p);
+  return launch_kernel(shared_merge_kernel<1, kMode>, dim3((unsigned)((rows + per_block - 1) / per_block)),
+                       dim3(kMergeThreads), stream, p);
 }
 
 }  // namespace
 
-hipError_t launch_decode_shared(const SharedParams &p0, hipStream_t stream) {
-  SharedParams p = p0;
-  DecodeParams &d = p.d;
-  const bool wide_item = d.nq * d.group > kCols;
-  d.item_cols = wide_item ? 2 * kCols : kCols;
-  p.small = d.ns <= kWave && p.ng < kWave;
-  hipError_t e = p.small ? hipSuccess : launch_kernel(shared_plan_kernel, dim3(1), dim3(kPlanThreads), stream, p);
-  if (e != hipSuccess) return e;
-  e = wide_item ? launch_work<2>(p, stream) : launch_work<1>(p, stream);
-  if (e != hipSuccess) return e;
-  const int64_t rows = (int64_t)d.ns * d.nq * d.hq;
-  constexpr int per_block = kMergeThreads / kWave;
-  if (rows <= kWideMergeRows)
-    return launch_kernel(shared_merge_kernel<per_block>, dim3((unsigned)rows), dim3(kMergeThreads), stream, p);
-  return launch_kernel(shared_merge_kernel<1>, dim3((unsigned)((rows + per_block - 1) / per_block)),
-                       dim3(kMergeThreads), stream, p);
+hipError_t launch_decode_shared(const SharedParams &p, hipStream_t stream) {
+  return p.d.nq * p.d.group > kCols ? launch_cg<2, kSuffix>(p, stream) : launch_cg<1, kSuffix>(p, stream);
+}
+
+hipError_t launch_decode_shared_scored(const SharedParams &p, hipStream_t stream) {
+  return launch_cg<2, kSuffixScored>(p, stream);  // (more than kKeepColumns columns)
 }
 
 }  // namespace hswa

@@ -125,7 +125,7 @@ struct SharedHead {
 };
 struct SharedParams {
   DecodeParams d;              // the own keys; start, own_units and own point into the plan
-  const int32_t *cu_groups;    // [ng + 1]
+  const int32_t *cu_groups;    // [ng + 1], or null: every sequence is a group, all it can share
   const int32_t *shared_lens;  // [ng]
   int32_t ng, max_shared;
   int32_t small;               // the workgroups find the plan (set at launch)
@@ -138,6 +138,22 @@ struct SharedParams {
   int32_t *group_of;     // [ns]
   float *ws_o;           // partial rows of the prefixes
   float *ws_lse;
+};
+
+// Decode that also adds every key's attention weight to a score (decode_scored.hip).
+// Up to this many (query, head) columns of a KV head the scores are stored, 4
+// bytes for each of a key's columns. 64 / 8 heads, 16 sequences, us a call with
+// them stored and formed anew: 24 columns (3 queries) over 2 - 16K keys 186 and
+// 222, over 30 - 32K 558 and 586; 32 columns 205 and 225, 620 and 592; one
+// sequence of 4K 31 and 27, 34 and 33. From there on it is the workspace that
+// counts: 32 columns of 16 x 64K keys take 1.1 GB.
+constexpr int kKeepColumns = 16;
+struct ScoredParams {
+  SharedParams s;          // s.d: split, with ws_s; or with row_lse, all of s, each sequence a group
+  const float *scores_in;  // [ns][Hkv][stride], or null for zeros; may be scores_out
+  float *scores_out;
+  int64_t stride;
+  int64_t merge_blocks;    // workgroups that merge rows (set at launch)
 };
 
 // Eviction (kv_evict.hip): keys of `src` kept by score move to the pages of `dst`.
@@ -153,18 +169,10 @@ struct EvictParams {
   int32_t ns, hkv, max_ctx, max_keep, num_recent, num_sinks;
 };
 
-// Decode that also adds every key's attention weight to a score (decode_scored.hip).
-constexpr int kKeepColumns = 32;  // up to this many (query, head) columns of a KV head the scores are stored
-struct ScoredParams {
-  DecodeParams d;          // split (max_splits > 1), with ws_s or row_lse
-  const float *scores_in;  // [ns][Hkv][stride], or null for zeros; may be scores_out
-  float *scores_out;
-  int64_t stride;
-  int64_t merge_blocks;    // workgroups that merge rows (set at launch)
-};
-
 hipError_t launch_kv_append(const AppendParams &p, hipStream_t stream);
 hipError_t launch_decode_shared(const SharedParams &p, hipStream_t stream);
+// The same with fp32 row sums, leaving the rows' log2 sum-exps in d.row_lse.
+hipError_t launch_decode_shared_scored(const SharedParams &p, hipStream_t stream);
 hipError_t launch_decode_scored(const ScoredParams &p, hipStream_t stream);
 hipError_t launch_kv_evict(const EvictParams &p, hipStream_t stream);
 hipError_t launch_decode(const DecodeParams &p, hipStream_t stream);

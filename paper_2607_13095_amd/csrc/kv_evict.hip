@@ -223,7 +223,8 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictParams p)
   __shared__ int s_page[kSlots], s_off[kSlots];  // source page (-1: none) and offset of each slot
   __shared__ int s_block[kSlots];                // its block, numbered among those of this workgroup
   __shared__ int s_first[kSlots + 1];            // first slot of each block
-  __shared__ int s_blocks;
+  __shared__ int s_to[kSlots];                   // page of each slot (-1: none)
+  __shared__ int s_blocks, s_count;
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int64_t chunks = (p.max_keep + kSlots - 1) / kSlots, total = chunks * p.ns * p.hkv;
   const int pgm = (1 << p.src.pg_shift) - 1;
@@ -231,15 +232,21 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictParams p)
     const int64_t row = item / chunks;
     const int b = (int)(row / p.hkv), g = (int)(row - (int64_t)b * p.hkv);
     const int s0 = (int)(item - row * chunks) * kSlots;
-    const int n = min(p.new_lens[b] - s0, kSlots);  // slots of this workgroup
-    if (n <= 0) continue;  // (the same for every thread)
-    __syncthreads();
+    __syncthreads();  // (the arrays have been read for the item before)
     if (wave == 0) {
-      const bool in = lane < n;
-      const int j = in ? p.kept[row * p.max_keep + s0 + lane] : 0;
+      // the loads that need no other go out together: the length, the kept
+      // positions (whatever lies behind them), the pages of the new slots
+      const int len = p.new_lens[b];
+      const int at = s0 + (lane & (kSlots - 1));
+      int j = at < p.max_keep ? p.kept[row * p.max_keep + at] : 0;
+      const int to = page_of(p.dst, b, at);
+      const int count = min(len - s0, kSlots);
+      const bool in = lane < count;
+      j = in ? j : 0;
       const int before = __shfl_up(j, 1, kWave);
       const uint64_t starts = __ballot(in && (lane == 0 || j / kB != before / kB));
       if (lane < kSlots) {
+        s_to[lane] = in ? to : -1;
         s_page[lane] = in ? page_of(p.src, b, j) : -1;
         s_off[lane] = j & pgm;
         const int blk = __popcll(starts & (((uint64_t)2 << lane) - 1)) - 1;
@@ -248,10 +255,13 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictParams p)
       }
       if (lane == 0) {
         s_blocks = __popcll(starts);
-        s_first[__popcll(starts)] = n;
+        s_first[__popcll(starts)] = count;
+        s_count = count;
       }
     }
     __syncthreads();
+    const int n = s_count;  // slots of this workgroup
+    if (n <= 0) continue;
     const u32x4 z = {0u, 0u, 0u, 0u};
     // K: pieces in the order of the new block, so that stores are whole runs
     constexpr int rb = kB == 32 ? 4 : 3;  // log2 of the rows of a half block
@@ -261,7 +271,7 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictParams p)
       const int r = x & ((1 << rb) - 1), piece = (x >> rb) & 3, slab = (x >> (rb + 2)) & 3, half = (x >> (rb + 4)) & 1;
       const int i = ((x >> (rb + 5)) << (rb + 1)) + 8 * (r >> 2) + 4 * half + (r & 3);
       const int d = 32 * slab + 8 * piece;
-      const int to = i < n ? page_of(p.dst, b, s0 + i) : -1;
+      const int to = s_to[i];
       if (to < 0) continue;
       const u32x4 v = s_page[i] >= 0 ? ldg128(p.src.k_pool + k_offset(p.src, s_page[i], p.hkv, g, s_off[i], d)) : z;
       stg128(p.dst.k_pool + k_offset(p.dst, to, p.hkv, g, (s0 + i) & pgm, d), v);
@@ -300,7 +310,7 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictParams p)
       }
       __builtin_amdgcn_wave_barrier();
     }
-    const int to = i0 < n ? page_of(p.dst, b, s0 + i0) : -1;
+    const int to = s_to[i0];
     if (to >= 0) {
       uint16_t *dst = p.dst.v_pool + v_offset(p.dst, to, p.hkv, g, (s0 + i0) & pgm, d);
 #pragma unroll
