@@ -49,8 +49,8 @@ __device__ __forceinline__ Keep keep_of(const EvictParams &p, int b) {
 // Scores as whole numbers in the same order (the two zeros are equal; a NaN
 // counts as -infinity).
 __device__ __forceinline__ uint32_t score_key(float s) {
-  const uint32_t u = __builtin_bit_cast(uint32_t, s != s ? -INFINITY : s + 0.f);
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
+  const uint32_t u = __builtin_bit_cast(uint32_t, fmaxf(s + 0.f, -INFINITY));
+  return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 
 // kPer: scores that a thread holds in registers, 64 positions of a wave apart; 0:
@@ -102,18 +102,32 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictParam
         f(i, score_key(held[e]), held[e], i < w1);
       }
     } else {
-      for (int i0 = w0; i0 < w1; i0 += kBatch * kWave) {
-        float s[kBatch];
+      // the next batch's loads go out before this one is worked on; whole batches
+      // need no bounds
+      auto load = [&](int i0, float (&s)[kBatch]) {
 #pragma unroll
         for (int e = 0; e < kBatch; ++e) {
           const int i = i0 + e * kWave + lane;
           s[e] = i < w1 ? scores[i] : 0.f;
         }
+      };
+      float next[kBatch];
+      load(w0, next);
+      for (int i0 = w0; i0 < w1; i0 += kBatch * kWave) {
+        float s[kBatch];
 #pragma unroll
-        for (int e = 0; e < kBatch; ++e) {
-          if (i0 + e * kWave >= w1) break;
-          const int i = i0 + e * kWave + lane;
-          f(i, score_key(s[e]), s[e], i < w1);
+        for (int e = 0; e < kBatch; ++e) s[e] = next[e];
+        load(i0 + kBatch * kWave, next);
+        if (i0 + kBatch * kWave <= w1) {
+#pragma unroll
+          for (int e = 0; e < kBatch; ++e) f(i0 + e * kWave + lane, score_key(s[e]), s[e], true);
+        } else {
+#pragma unroll
+          for (int e = 0; e < kBatch; ++e) {
+            if (i0 + e * kWave >= w1) break;
+            const int i = i0 + e * kWave + lane;
+            f(i, score_key(s[e]), s[e], i < w1);
+          }
         }
       }
     }
