@@ -133,7 +133,7 @@ DecodeGeometry decode_geometry(const hswa_shape *sh, int32_t ns, int32_t max_ctx
 // prefixes.
 struct SharedGeometry {
   DecodeGeometry d;
-  size_t groups, group_units, group_rows, own_units, start, group_of, own, ws_o, ws_lse, total_bytes;
+  size_t groups, group_units, group_rows, own_units, start, group_of, seqs, own, ws_o, ws_lse, total_bytes;
 };
 
 SharedGeometry shared_geometry(const hswa_shape *sh, int32_t ns, int32_t max_ctx, int32_t nq, int32_t ng) {
@@ -152,6 +152,7 @@ SharedGeometry shared_geometry(const hswa_shape *sh, int32_t ns, int32_t max_ctx
   g.own_units = take((size_t)ns * sizeof(int64_t));
   g.start = take((size_t)ns * sizeof(int32_t));
   g.group_of = take((size_t)ns * sizeof(int32_t));
+  g.seqs = take((size_t)ns * sizeof(hswa::SharedSeq));
   g.own = take(g.d.total_bytes);
   // a piece of a prefix has the rows of its columns, in 16s for a group's; each span adds at most a
   // workgroup's columns
@@ -242,6 +243,7 @@ void shared_params(hswa::SharedParams &p, const SharedGeometry &geo, int32_t num
   p.own_units = reinterpret_cast<int64_t *>(ws + geo.own_units);
   p.start = reinterpret_cast<int32_t *>(ws + geo.start);
   p.group_of = reinterpret_cast<int32_t *>(ws + geo.group_of);
+  p.seqs = reinterpret_cast<hswa::SharedSeq *>(ws + geo.seqs);
   p.ws_o = reinterpret_cast<float *>(ws + geo.ws_o);
   p.ws_lse = reinterpret_cast<float *>(ws + geo.ws_lse);
   p.d.start = p.start;

@@ -37,7 +37,7 @@
 namespace hswa {
 namespace {
 
-constexpr int kPlanThreads = 1024;
+constexpr int kPlanThreads = 256;
 constexpr int kPlanWaves = kPlanThreads / kWave;
 constexpr int kGroupLanes = 16;     // lanes that look over a group's sequences
 constexpr int kThreads = 512;
@@ -69,20 +69,20 @@ __device__ __forceinline__ int64_t ceil_div(int64_t a, int64_t b) {  // a >= 0, 
   if (((a + b) >> 31) == 0) return ((uint32_t)a + (uint32_t)b - 1) / (uint32_t)b;  // (much shorter)
   return (a + b - 1) / b;
 }
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {  // likewise
+  return ((a | b) >> 31) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
 
 // Inclusive scan over the workgroup of the plan with `op`; `last`: the result of all.
 template <typename Op>
 __device__ __forceinline__ int64_t block_scan(int64_t x, int64_t (&part)[kPlanWaves], int64_t &last, Op op) {
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-#pragma unroll
-  for (int off = 1; off < kWave; off <<= 1) {
-    const int64_t t = __shfl_up(x, off, kWave);
-    if (lane >= off) x = op(x, t);
-  }
+  x = wave_scan(x, (int64_t)0, op);  // (sums and maxima of what is not negative)
   __syncthreads();  // (part was read by the scan before)
   if (lane == kWave - 1) part[wave] = x;
   __syncthreads();
   last = part[0];
+#pragma unroll
   for (int w = 1; w < kPlanWaves; ++w) {
     if (w == wave) x = op(x, last);
     last = op(last, part[w]);
@@ -244,10 +244,21 @@ __device__ __forceinline__ void plan_small(const SharedParams &p, SmallPlan &at)
     p.group_units[lane] = at.units[lane] = units;
     p.group_rows[lane] = at.rows[lane] = rows;
   }
+  // (the exchanges need every lane)
+  SharedSeq q;
+  const int from = max(grp, 0), first = __shfl(g.first, from, kWave);
+  q.start = start;
+  q.col = (lane - first) * d.nq * d.group;
+  q.tiles = tiles;
+  q.padded = __shfl(g.padded, from, kWave);
+  q.cols = __shfl(g.cols, from, kWave);
+  q.units = __shfl(units, from, kWave);
+  q.rows = __shfl(rows, from, kWave);
+  q.own_units = before;
   if (lane < d.ns) {
     p.start[lane] = start;
-    p.group_of[lane] = tiles > 0 ? grp : -1;
     p.own_units[lane] = before;
+    p.seqs[lane] = q;
   }
   if (lane == 0) {
     p.group_units[p.ng] = at.units[p.ng] = h.units;
@@ -344,24 +355,42 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(SharedParams 
     chunks += total;
     longest = max64(longest, m);
   }
-  if (tid >= kWave) return;
-  SharedHead h;
-  if (p.ng < kWave) {  // few groups: as in a small plan
-    SharedGroup g{};
-    if (tid < p.ng) g = p.groups[tid];
-    int64_t before, first;
-    h = plan_groups(p, g, chunks * H, longest, before, first);
-    if (tid < p.ng) {
-      p.groups[tid] = g;
-      p.group_units[tid] = before;
-      p.group_rows[tid] = first;
+  if (tid < kWave) {
+    SharedHead h;
+    if (p.ng < kWave) {  // few groups: as in a small plan
+      SharedGroup g{};
+      if (tid < p.ng) g = p.groups[tid];
+      int64_t before, first;
+      h = plan_groups(p, g, chunks * H, longest, before, first);
+      if (tid < p.ng) {
+        p.groups[tid] = g;
+        p.group_units[tid] = before;
+        p.group_rows[tid] = first;
+      }
+    } else {
+      h = divide_work(d, units, cost, chunks * H, longest);
     }
-  } else {
-    h = divide_work(d, units, cost, chunks * H, longest);
+    if (tid == 0) {
+      p.group_units[p.ng] = h.units;
+      *p.head = h;
+    }
   }
-  if (tid == 0) {
-    p.group_units[p.ng] = h.units;
-    *p.head = h;
+  __syncthreads();
+  for (int b = tid; b < d.ns; b += kPlanThreads) {
+    SharedSeq q{};
+    q.start = p.start[b];
+    q.own_units = p.own_units[b];
+    if (q.start > 0) {
+      const int i = p.group_of[b];
+      const SharedGroup g = p.groups[i];
+      q.col = (b - g.first) * d.nq * d.group;
+      q.tiles = g.tiles;
+      q.padded = g.padded;
+      q.cols = g.cols;
+      q.units = p.group_units[i];
+      q.rows = p.group_rows[i];
+    }
+    p.seqs[b] = q;
   }
 }
 
@@ -756,35 +785,48 @@ __global__ __launch_bounds__(kMergeThreads) void shared_merge_kernel(SharedParam
     if (scored(kMode) && lane == 0) d.row_lse[idx] = INFINITY;
     return;
   }
+  const SharedHead h = *p.head;
+  const SharedSeq seq = p.seqs[b];
   const int rem = (int)(idx - (int64_t)b * d.nq * d.hq);
   const int qi = rem / d.hq, head = rem - qi * d.hq;
   const int g = head / d.group, hh = head - g * d.group;
   // pieces of the prefix: rows first, first + 256, ... of its partials
   int n0 = 0;
   int64_t first = 0;
-  const int start = p.start[b];
-  if (start > 0) {
-    const int gi = p.group_of[b];
-    const SharedGroup grp = p.groups[gi];
-    const int col = ((b - grp.first) * d.nq + qi) * d.group + hh;
-    const int ntc = (grp.cols + kTileCols - 1) / kTileCols;
-    const int64_t seg = p.group_units[gi] + (int64_t)(g * ntc + col / kTileCols) * grp.padded;
-    const int64_t s0 = seg / p.head->per, s1 = (seg + grp.tiles - 1) / p.head->per;
-    n0 = (int)(s1 - s0) + 1;
-    first = p.group_rows[gi] + (int64_t)g * ((grp.cols + kCols - 1) / kCols * kCols) + col + s0 * kTileCols;
+  if (seq.start > 0) {
+    const int col = seq.col + qi * d.group + hh;
+    const int ntc = (seq.cols + kTileCols - 1) / kTileCols;
+    const int64_t u = seq.units + (int64_t)(g * ntc + col / kTileCols) * seq.padded;
+    const int64_t s0 = quotient(u, h.per);
+    n0 = (int)(quotient(u + seq.tiles - 1, h.per) - s0) + 1;
+    first = seq.rows + (int64_t)g * ((seq.cols + kCols - 1) / kCols * kCols) + col + s0 * kTileCols;
   }
   // and of its own keys
-  const int nch = (ctx - start + kChunk - 1) / kChunk;
+  const int nch = (ctx - seq.start + kChunk - 1) / kChunk;
   int n1 = 0;
   if (nch > 0) {
-    const int hchunks = (d.nq * d.group + d.item_cols - 1) / d.item_cols;
-    const OwnSpans own = p.head->own;
-    const int64_t pitch = own.aligned ? (nch + own.per - 1) / own.per * own.per : nch;
-    const int64_t seg = p.own_units[b] + (g * hchunks + (qi * d.group + hh) / d.item_cols) * pitch;
-    n1 = (int)((seg + nch - 1) / own.per - seg / own.per) + 1;
+    if (h.own.aligned) {
+      n1 = (int)ceil_div(nch, h.own.per);
+    } else {
+      const int hchunks = (d.nq * d.group + d.item_cols - 1) / d.item_cols;
+      const int64_t u = seq.own_units + (int64_t)(g * hchunks + (qi * d.group + hh) / d.item_cols) * nch;
+      n1 = (int)(quotient(u + nch - 1, h.own.per) - quotient(u, h.own.per)) + 1;
+    }
   }
   if (!scored(kMode) && n0 == 0 && n1 == 1) return;  // one piece: the decode kernel wrote the row
   const int n = n0 + n1;
+  const float *po0 = p.ws_o + first * kHeadDim + d4, *po1 = d.ws_o + idx * d.max_splits * kHeadDim + d4;
+  auto load = [&](int s0, f32x4 (&v)[8]) {  // pieces s0 .. s0 + 15
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int s = s0 + 2 * k + half;
+      const f32x4 z = {0.f, 0.f, 0.f, 0.f};
+      const float *src = s < n0 ? po0 + (int64_t)s * kTileCols * kHeadDim : po1 + (int64_t)(s - n0) * kHeadDim;
+      v[k] = s < n ? *reinterpret_cast<const f32x4 *>(src) : z;
+    }
+  };
+  f32x4 v[8];
+  load(16 * rw, v);  // (beside the log-sum-exps)
   auto lse_of = [&](int s) {
     return s < n0 ? p.ws_lse[first + (int64_t)s * kTileCols] : d.ws_lse[idx * d.max_splits + s - n0];
   };
@@ -798,7 +840,6 @@ __global__ __launch_bounds__(kMergeThreads) void shared_merge_kernel(SharedParam
     if (scored(kMode) && lane == 0) d.row_lse[idx] = INFINITY;
     return;
   }
-  const float *po0 = p.ws_o + first * kHeadDim + d4, *po1 = d.ws_o + (idx * d.max_splits - n0) * kHeadDim + d4;
   float wsum = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   for (int s0 = 0; s0 < n; s0 += kWave) {
@@ -806,21 +847,14 @@ __global__ __launch_bounds__(kMergeThreads) void shared_merge_kernel(SharedParam
     const float w = s < n ? fast_exp2(lse_of(s) - mx) : 0.f;
     const int m = min(kWave, n - s0);
     for (int k0 = 16 * rw; k0 < m; k0 += 16 * kRowWaves) {
-      f32x4 v[8];
+      if (s0 + k0 != 16 * rw) load(s0 + k0, v);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        const int pc = k0 + 2 * k + half, sp = s0 + pc;
-        const f32x4 z = {0.f, 0.f, 0.f, 0.f};
-        const float *src = sp < n0 ? po0 + (int64_t)sp * kTileCols * kHeadDim : po1 + (int64_t)sp * kHeadDim;
-        v[k] = pc < m ? *reinterpret_cast<const f32x4 *>(src) : z;
-      }
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int pc = k0 + 2 * k + half;
-        const float wk = __shfl(w, min(pc, kWave - 1), kWave);
-        const float wv = pc < m ? wk : 0.f;
-        wsum += wv;
-        o += wv * v[k];
+        const float we = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), k0 + 2 * k));
+        const float wd = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), k0 + 2 * k + 1));
+        const float wk = half ? wd : we;  // (0 past the last piece)
+        wsum += wk;
+        o += wk * v[k];
       }
     }
   }

@@ -117,6 +117,14 @@ struct SharedGroup {
   int32_t padded;  // units that they take in the order of spans
   int32_t cols;    // columns of a KV head (0 without tiles)
 };
+// What the merge needs of a sequence.
+struct SharedSeq {
+  int32_t start;           // shared keys
+  int32_t col;             // its first column in its group's
+  int32_t tiles, padded, cols;  // of its group
+  int64_t units, rows;     // before its group
+  int64_t own_units;
+};
 struct SharedHead {
   int64_t units;    // key tiles of all (group, KV head, kSharedCols columns), padded
   int64_t per;      // of them, those of a span
@@ -135,7 +143,8 @@ struct SharedParams {
   int64_t *group_rows;   // [ng] rows of partials before each group
   int64_t *own_units;    // [ns] units of own keys (of every KV head) before each sequence's
   int32_t *start;        // [ns] shared keys of each sequence
-  int32_t *group_of;     // [ns]
+  int32_t *group_of;     // [ns] (batches whose plan is a kernel)
+  SharedSeq *seqs;       // [ns]
   float *ws_o;           // partial rows of the prefixes
   float *ws_lse;
 };
