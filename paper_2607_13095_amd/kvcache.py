@@ -47,3 +47,43 @@ class LayerKV:
 
     def nbytes(self) -> int:
         return 2 * self.num_pages * hswa.page_bytes(self.shape)
+
+
+def prefix_groups(table, context_lens: Sequence[int], page_size: int):
+    """Groups for ``hswa.decode_shared`` from a batch's host block table [NS,
+    stride]: runs of consecutive sequences whose rows name the same leading
+    pages, chosen so that the positions read once instead of several times,
+    sum (n - 1) * shared over the groups, are the most. Returns (cu_groups,
+    shared_lens) as int32 arrays; a sequence that shares nothing is a group of its
+    own, of shared length 0. Sequences that share a prefix have to stand next to
+    each other (sort a batch by its first pages); a page counts as shared as far
+    as the shortest context of its group fills it.
+    """
+    table, lens = np.asarray(table), [int(x) for x in context_lens]
+    ns, pg = len(lens), int(page_size)
+    # positions that neighbours share
+    common = []
+    for b in range(ns - 1):
+        n = min(-(-min(lens[b], lens[b + 1]) // pg), table.shape[1])
+        same = (table[b, :n] == table[b + 1, :n]) & (table[b, :n] >= 0)
+        pages = n if same.all() else int(np.argmin(same))
+        common.append(min(pages * pg, lens[b], lens[b + 1]))
+    best, cut = [0] * (ns + 1), list(range(-1, ns))  # of the sequences before each one; where its last group starts
+    for end in range(1, ns + 1):
+        best[end], cut[end] = best[end - 1], end - 1
+        least = None
+        for first in range(end - 2, -1, -1):
+            least = common[first] if least is None else min(least, common[first])
+            if least <= 0:
+                break
+            saved = best[first] + (end - 1 - first) * least
+            if saved > best[end]:
+                best[end], cut[end] = saved, first
+    starts = []
+    end = ns
+    while end > 0:
+        starts.append(cut[end])
+        end = cut[end]
+    cu = starts[::-1] + [ns]
+    shared = [min(common[a:b - 1]) if b - a > 1 else 0 for a, b in zip(cu[:-1], cu[1:])]
+    return np.asarray(cu, dtype=np.int32), np.asarray(shared, dtype=np.int32)
