@@ -173,20 +173,30 @@ __global__ __launch_bounds__(kScoreThreads) void scored_finish_kernel(ScoredPara
     const int64_t seg = uni64(before) * p.hkv + (int64_t)g * nch;
     const int pieces = (int)((seg + nch - 1) / per - seg / per) + 1;
     __syncthreads();  // (s_lse of the item before has been read)
-    for (int c = wave; c < ncols; c += kScoreThreads / kWave) {
-      const int qi = c / p.group;
-      const int64_t row = ((int64_t)b * p.nq + qi) * p.hq + (int64_t)g * p.group + (c - qi * p.group);
-      const float *lse = p.ws_lse + row * p.max_splits;
-      float mx = -INFINITY;
-      for (int s = lane; s < pieces; s += kWave) mx = fmaxf(mx, lse[s]);
+    // the columns' log-sum-exps: four a wave (kKeepColumns = 16), their loads together
+    constexpr int kEach = kKeepColumns / (kScoreThreads / kWave);
+    const float *lse[kEach];
+    float first[kEach];
 #pragma unroll
-      for (int off = 1; off < kWave; off <<= 1) mx = fmaxf(mx, __shfl_xor(mx, off, kWave));
-      float sum = 0.f;
-      for (int s = lane; s < pieces; s += kWave) sum += fast_exp2(lse[s] - mx);
+    for (int e = 0; e < kEach; ++e) {
+      const int c = min(wave + e * (kScoreThreads / kWave), ncols - 1), qi = c / p.group;
+      lse[e] = p.ws_lse + (((int64_t)b * p.nq + qi) * p.hq + (int64_t)g * p.group + (c - qi * p.group)) * p.max_splits;
+      first[e] = lane < pieces ? lse[e][lane] : -INFINITY;
+    }
 #pragma unroll
-      for (int off = 1; off < kWave; off <<= 1) sum += __shfl_xor(sum, off, kWave);
+    for (int e = 0; e < kEach; ++e) {
+      const auto most = [](float a, float b) { return fmaxf(a, b); };
+      const auto add = [](float a, float b) { return a + b; };
+      float mx = first[e];
+      for (int s = lane + kWave; s < pieces; s += kWave) mx = fmaxf(mx, lse[e][s]);
+      mx = last_lane(wave_scan(mx, -INFINITY, most));
       // (a row that sees no key has scores of -infinity: weight 0 under any finite or +infinite sum)
-      if (lane == 0) s_lse[c] = mx == -INFINITY ? INFINITY : mx + __log2f(sum);
+      const float base = mx == -INFINITY ? 0.f : mx;
+      float sum = fast_exp2(first[e] - base);
+      for (int s = lane + kWave; s < pieces; s += kWave) sum += fast_exp2(lse[e][s] - base);
+      sum = last_lane(wave_scan(sum, 0.f, add));
+      const int c = wave + e * (kScoreThreads / kWave);
+      if (lane == 0 && c < ncols) s_lse[c] = mx == -INFINITY ? INFINITY : mx + __log2f(sum);
     }
     __syncthreads();
     const int j = k0 + 4 * tid;

@@ -109,8 +109,7 @@ __device__ __forceinline__ SharedHead divide_work(const DecodeParams &d, int64_t
     const float own_per = fmaxf((float)kMinOwn, ceilf(o / (max(kSharedSpans - mine, 1) * kWorkWaves)));
     const float own = o == 0.f ? 0.f : mine == kSharedSpans ? FLT_MAX : kCostOwnStart + fmaxf(own_per * kCostOwn, o * kCostOwnHbm);
     const float t = fmaxf(kCostSpan + per * ((float)cost / u), own) + mine * kCostMerge;
-    const float scan = wave_scan(t, FLT_MAX, [](float a, float b) { return fminf(a, b); });
-    const float least = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, scan), kWave - 1));
+    const float least = last_lane(wave_scan(t, FLT_MAX, [](float a, float b) { return fminf(a, b); }));
     n = kXcds * (__builtin_ctzll(__ballot(t == least)) + 1);
   }
   SharedHead h;

@@ -168,6 +168,10 @@ __device__ __forceinline__ T wave_scan(T x, T none, Op op) {
   x = op(x, lane_move<0x143, 0xc>(none, x));  // lane 31 to the upper rows
   return x;
 }
+__device__ __forceinline__ float last_lane(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), kWave - 1));
+}
+
 
 constexpr float kLog2e = 1.4426950408889634f;
 

@@ -28,7 +28,6 @@ constexpr int kBatch = 16;
 constexpr int kCopies = 4;  // of the histogram, for lanes that meet in a bin
 constexpr int kMoveThreads = 256;
 constexpr int kSlots = 32;        // slots of the new pages per workgroup of the move
-constexpr int kStageBlocks = 4;   // V blocks a wave holds in LDS (a power of two)
 constexpr int kMaxMoveGrid = 1 << 20;
 
 // What a sequence keeps, by count: its first and last keys and those picked by
@@ -58,6 +57,7 @@ __device__ __forceinline__ uint32_t score_key(float s) {
 // (one at a time a pass over 58K scores took 20 us; 64 held spilled).
 template <int kPer>
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictParams p) {
+  constexpr int kEach = kBins / kSelectThreads;  // bins of a thread
   __shared__ uint32_t hist[kBins * kCopies];
   __shared__ uint32_t wsum[2][kSelectWaves];
   __shared__ uint32_t found[3];
@@ -145,29 +145,31 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictParam
       if (in && (k & known) == top) atomicAdd(&hist[((k >> shift) & digit) * kCopies + (lane & (kCopies - 1))], 1u);
     });
     __syncthreads();
-    // the bins from the highest down, two a thread: where the count reaches `need`
-    const int hb = kBins - 1 - 2 * tid;
-    uint32_t c0 = 0, c1 = 0;
+    // the bins from the highest down, kEach a thread: where the count reaches `need`
+    const int hb = kBins - 1 - kEach * tid;
+    uint32_t count[kEach], s = 0;
 #pragma unroll
-    for (int c = 0; c < kCopies; ++c) {
-      c0 += hist[hb * kCopies + c];
-      c1 += hist[(hb - 1) * kCopies + c];
-    }
-    uint32_t s = c0 + c1;
+    for (int e = 0; e < kEach; ++e) {
+      count[e] = 0;
 #pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) {
-      const uint32_t t = __shfl_up(s, off, kWave);
-      if (lane >= off) s += t;
+      for (int c = 0; c < kCopies; ++c) count[e] += hist[(hb - e) * kCopies + c];
+      s += count[e];
     }
+    const uint32_t mine = s;
+    s = wave_scan(s, 0u, [](uint32_t a, uint32_t b) { return a + b; });
     if (lane == kWave - 1) wsum[0][wave] = s;
     __syncthreads();
-    uint32_t before = s - c0 - c1;
-    for (int w = 0; w < wave; ++w) before += wsum[0][w];
-    if (before < need && need <= before + c0 + c1) {
-      const bool first = need <= before + c0;
-      found[0] = first ? hb : hb - 1;
-      found[1] = first ? before : before + c0;
-      found[2] = first ? c0 : c1;
+    uint32_t before = s - mine;
+#pragma unroll
+    for (int w = 0; w < kSelectWaves; ++w) before += w < wave ? wsum[0][w] : 0u;
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      if (before < need && need <= before + count[e]) {
+        found[0] = hb - e;
+        found[1] = before;
+        found[2] = count[e];
+      }
+      before += count[e];
     }
     __syncthreads();
     need -= found[1];
@@ -224,9 +226,9 @@ __device__ __forceinline__ int page_of(const PoolView &pv, int b, int j) {
 // 32 slots of the new pages. K moves in 16-byte pieces (8 dims of a key). V is
 // stored with a block's keys side by side, so a kept key is 2 bytes here and
 // there: each wave takes 32 dims, loads whole rows of the blocks that hold kept
-// keys (kStageBlocks at a time, in LDS) and picks from them the 16 slots of a
-// lane's dim. kB: keys of a block (16 for 16-key pages, else 32).
-template <int kB>
+// keys (kStageBlocks, a power of two, at a time, in LDS) and picks from them the
+// 16 slots of a lane's dim. kB: keys of a block (16 for 16-key pages, else 32).
+template <int kB, int kStageBlocks>
 __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictParams p) {
   constexpr int kDims = kHeadDim / (kMoveThreads / kWave);  // dims of a wave
   constexpr int kRow = 2 * kB / 16;                         // 16-byte pieces of a block's row
@@ -353,8 +355,15 @@ hipError_t launch_kv_evict(const EvictParams &p, hipStream_t stream) {
   if (e != hipSuccess) return e;
   const int64_t items = (int64_t)((p.max_keep + kSlots - 1) / kSlots) * p.ns * p.hkv;
   const dim3 grid((unsigned)std::min<int64_t>(items, kMaxMoveGrid)), block(kMoveThreads);
-  return p.src.vb_shift == 4 ? launch_kernel(evict_move_kernel<16>, grid, block, stream, p)
-                             : launch_kernel(evict_move_kernel<32>, grid, block, stream, p);
+  // With a workgroup per compute unit or fewer, more blocks at a time save waits
+  // (1 x 4K to 1024, 8 KV heads: 9.7 and 8.5 us); with more of them, four leave
+  // room in LDS for three on a unit (16 x 16K: 194 us, with eight 340).
+  const bool few = items <= 256;
+  if (p.src.vb_shift == 4)
+    return few ? launch_kernel(evict_move_kernel<16, 8>, grid, block, stream, p)
+               : launch_kernel(evict_move_kernel<16, 4>, grid, block, stream, p);
+  return few ? launch_kernel(evict_move_kernel<32, 8>, grid, block, stream, p)
+             : launch_kernel(evict_move_kernel<32, 4>, grid, block, stream, p);
 }
 
 }  // namespace hswa

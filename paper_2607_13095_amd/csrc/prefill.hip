@@ -136,10 +136,6 @@ struct Walk {
   int64_t next;   // where the query tile at u ends (u1 if the span ends in it)
 };
 
-__device__ __forceinline__ float last_lane(float x) {
-  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), kWave - 1));
-}
-
 // Whether cutting the call into spans gains, by its lengths (lane b holds
 // sequence b; every wave finds it by itself). In key tiles, a query tile worth
 // its key tiles plus kTileCost, the unsplit call takes the largest of: the load
