@@ -7,4 +7,5 @@ the dual pools and block tables with PyTorch device memory.
 
 from . import hswa  # noqa: F401
 from .hswa import (Cache, HswaError, Layer, Shape, build_block_table, decode,  # noqa: F401
-                   decode_split_len, decode_workspace_bytes, kv_append, load, page_bytes, prefill, ring_pages)
+                   decode_scored, decode_scored_workspace_bytes, decode_shared, decode_shared_workspace_bytes,
+                   decode_split_len, decode_workspace_bytes, kv_append, kv_evict, load, page_bytes, prefill, ring_pages)
