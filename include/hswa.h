@@ -351,7 +351,9 @@ hswa_status hswa_decode_multi(hswa_layer layer, const hswa_shape *shape, const h
  * hswa_decode_shared_workspace_bytes (FULL only). The call is hswa_decode_multi's,
  * bit for bit, where reading the prefixes once cannot gain: an SWA layer (it reads
  * its window), no group, one sequence, prefixes below 64, and calls whose
- * (ns - num_groups) * max_shared_len positions hold less than 70 MB.
+ * (ns - num_groups) * max_shared_len positions hold less than 70 MB, or whose
+ * max_context_len is over 2^30. HSWA_ERR_UNSUPPORTED beside hswa_decode_multi's:
+ * over 2^25 rows (ns * num_queries * Hq) in any other call.
  * The other arguments are as in hswa_decode_multi. */
 size_t hswa_decode_shared_workspace_bytes(const hswa_shape *shape, int32_t ns, int32_t num_queries,
                                           int32_t max_context_len, int32_t num_groups, int32_t max_shared_len);
@@ -378,7 +380,8 @@ hswa_status hswa_decode_shared(hswa_layer layer, const hswa_shape *shape, const 
  * The other arguments and the output rows are as in hswa_decode_multi (rows may
  * differ from its in the last bit: their sums are not of rounded probabilities);
  * workspace >= hswa_decode_scored_workspace_bytes, for contexts of any length.
- * SWA layers return HSWA_ERR_UNSUPPORTED: they evict by their window. */
+ * HSWA_ERR_UNSUPPORTED: an SWA layer (it evicts by its window), more than 2^25
+ * rows (ns * num_queries * Hq), a max_context_len over 2^30. */
 size_t hswa_decode_scored_workspace_bytes(const hswa_shape *shape, int32_t ns, int32_t num_queries,
                                           int32_t max_context_len);
 hswa_status hswa_decode_scored(hswa_layer layer, const hswa_shape *shape, const hswa_cache *cache, const void *q,
@@ -413,7 +416,8 @@ hswa_status hswa_decode_scored(hswa_layer layer, const hswa_shape *shape, const 
  * slots of `dst` from K_b on, are left as they were. new_lens_out: device int32
  * [ns], receives K_b. A kept position whose page id is not in the pool is
  * stored as a zero key and value, a slot whose page id is not is not stored.
- * HSWA_ERR_UNSUPPORTED: an SWA layer, or ns * Hkv of 2^22 and more.
+ * HSWA_ERR_UNSUPPORTED: an SWA layer, ns * Hkv of 2^22 and more, a
+ * max_context_len or kept_stride over 2^30.
  * HSWA_ERR_CAPACITY: a stride or a table too short for max_context_len or
  * kept_stride. */
 hswa_status hswa_kv_evict(hswa_layer layer, const hswa_shape *shape, const hswa_cache *src, const hswa_cache *dst,

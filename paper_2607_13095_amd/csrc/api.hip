@@ -35,6 +35,11 @@ constexpr int32_t kMaxKvHeads = 4096;
 // (sequence, KV head) pairs of a call with a workgroup of up to 1024 threads for each: a grid
 // holds less than 2^32 threads
 constexpr int32_t kMaxGridRows = (1 << 22) - 1;
+// (sequence, query, head) rows of the shared and scored decode, a merging wave for each, with
+// up to 2^28 threads more beside them
+constexpr int64_t kMaxRows = 1 << 25;
+// Positions of a sequence whose sums of keys, tiles and spans stay within 32 bits
+constexpr int32_t kMaxLen = 1 << 30;
 
 // Shape checks shared by every device call.
 hswa_status check_shape(const hswa_shape *sh) {
@@ -214,7 +219,7 @@ ScoredGeometry scored_geometry(const hswa_shape *sh, int32_t ns, int32_t max_ctx
 bool shared_fits(const hswa_shape *sh, int32_t ns, int32_t num_groups, int32_t max_context_len,
                  int32_t max_shared_len) {
   constexpr double kLeastSaved = 70e6;
-  if (ns < 2 || num_groups < 1 || max_shared_len < hswa::kSharedTile) return false;
+  if (ns < 2 || num_groups < 1 || max_shared_len < hswa::kSharedTile || max_context_len > kMaxLen) return false;
   const double keys = (double)(ns - num_groups) * (max_shared_len < max_context_len ? max_shared_len : max_context_len);
   return keys * sh->num_kv_heads * (sh->head_dim * 4) >= kLeastSaved;
 }
@@ -510,7 +515,8 @@ hswa_status hswa_decode_shared(hswa_layer layer, const hswa_shape *shape, const 
                                void *stream) {
   if (num_groups < 0 || max_shared_len < 0 || (ns >= 0 && num_groups > ns)) return HSWA_ERR_INVALID_ARG;
   if (num_groups > 0 && (!cu_groups || !shared_lens)) return HSWA_ERR_INVALID_ARG;
-  if (layer.kind != HSWA_LAYER_FULL || check_shape(shape) != HSWA_OK || !shared_fits(shape, ns, num_groups, max_context_len, max_shared_len))
+  if (layer.kind != HSWA_LAYER_FULL || check_shape(shape) != HSWA_OK ||
+      !shared_fits(shape, ns, num_groups, max_context_len, max_shared_len))
     return hswa_decode_multi(layer, shape, cache, q, context_lens, ns, num_queries, max_context_len, workspace,
                              workspace_bytes, out, stream);
   hswa_status st;
@@ -519,8 +525,7 @@ hswa_status hswa_decode_shared(hswa_layer layer, const hswa_shape *shape, const 
   if ((st = make_pool(layer, shape, cache, p.d.pool)) != HSWA_OK) return st;
   if ((int64_t)cache->table_stride * shape->page_size < (int64_t)max_context_len) return HSWA_ERR_CAPACITY;
   if (!q || !context_lens || !out || !workspace) return HSWA_ERR_INVALID_ARG;
-  // (column and row numbers of the plan are 32-bit)
-  if ((int64_t)ns * num_queries * shape->num_q_heads > INT32_MAX) return HSWA_ERR_UNSUPPORTED;
+  if ((int64_t)ns * num_queries * shape->num_q_heads > kMaxRows) return HSWA_ERR_UNSUPPORTED;
   const SharedGeometry geo = shared_geometry(shape, ns, max_context_len, num_queries, num_groups);
   if (workspace_bytes < geo.total_bytes) return HSWA_ERR_CAPACITY;
   decode_params(p.d, shape, q, context_lens, ns, num_queries, max_context_len, out);
@@ -535,7 +540,7 @@ hswa_status hswa_decode_shared(hswa_layer layer, const hswa_shape *shape, const 
 size_t hswa_decode_scored_workspace_bytes(const hswa_shape *shape, int32_t ns, int32_t num_queries,
                                           int32_t max_context_len) {
   if (check_shape(shape) != HSWA_OK || ns < 1 || max_context_len < 1) return 0;
-  if (num_queries < 1 || num_queries > kMaxQueries) return 0;
+  if (num_queries < 1 || num_queries > kMaxQueries || max_context_len > kMaxLen) return 0;
   return scored_geometry(shape, ns, max_context_len, num_queries).total_bytes;
 }
 
@@ -548,14 +553,14 @@ hswa_status hswa_decode_scored(hswa_layer layer, const hswa_shape *shape, const 
   if ((st = check_shape(shape)) != HSWA_OK) return st;
   if (layer.kind != HSWA_LAYER_FULL) return HSWA_ERR_UNSUPPORTED;
   if (ns < 0 || max_context_len < 1 || num_queries < 1 || num_queries > kMaxQueries) return HSWA_ERR_INVALID_ARG;
+  if (max_context_len > kMaxLen) return HSWA_ERR_UNSUPPORTED;
   hswa::ScoredParams p{};
   if ((st = make_pool(layer, shape, cache, p.s.d.pool)) != HSWA_OK) return st;
   if ((int64_t)cache->table_stride * shape->page_size < (int64_t)max_context_len) return HSWA_ERR_CAPACITY;
   if (score_stride < max_context_len) return HSWA_ERR_CAPACITY;
   if (ns == 0) return HSWA_OK;
   if (!q || !context_lens || !out || !scores_out || !workspace) return HSWA_ERR_INVALID_ARG;
-  // (column and row numbers are 32-bit)
-  if ((int64_t)ns * num_queries * shape->num_q_heads > INT32_MAX) return HSWA_ERR_UNSUPPORTED;
+  if ((int64_t)ns * num_queries * shape->num_q_heads > kMaxRows) return HSWA_ERR_UNSUPPORTED;
   const ScoredGeometry geo = scored_geometry(shape, ns, max_context_len, num_queries);
   if (workspace_bytes < geo.total_bytes) return HSWA_ERR_CAPACITY;
   decode_params(p.s.d, shape, q, context_lens, ns, num_queries, max_context_len, out);
@@ -587,6 +592,7 @@ hswa_status hswa_kv_evict(hswa_layer layer, const hswa_shape *shape, const hswa_
   if (layer.kind != HSWA_LAYER_FULL) return HSWA_ERR_UNSUPPORTED;
   if (ns < 0 || max_context_len < 1 || num_recent < 0 || num_sinks < 0 || kept_stride < 1) return HSWA_ERR_INVALID_ARG;
   if (ns > kMaxGridRows / shape->num_kv_heads) return HSWA_ERR_UNSUPPORTED;
+  if (max_context_len > kMaxLen || kept_stride > kMaxLen) return HSWA_ERR_UNSUPPORTED;
   hswa::EvictParams p{};
   if ((st = make_pool(layer, shape, src, p.src)) != HSWA_OK) return st;
   if ((st = make_pool(layer, shape, dst, p.dst)) != HSWA_OK) return st;

@@ -414,7 +414,7 @@ __device__ __forceinline__ void decode_waves(const DecodeParams &p, [[maybe_unus
       // that they go out in long runs: their bytes are a sixteenth of those read,
       // but writes between the reads cost HBM far more than that. 16 x 64K, 64 / 8
       // heads, us: 610 without the stores, 807 with a chunk's 1 KiB at a time, 797
-      // in runs of 16 KiB, 775 of 36 KiB, NNN written through past L2 (a line
+      // in runs of 16 KiB, 775 of 36 KiB, 740 written through past L2 (a line
       // held there is evicted in between some later reads).
       int kept = 0;
       int64_t kept_to = 0;  // where the next run goes, in 16-byte pieces

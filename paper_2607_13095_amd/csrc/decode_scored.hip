@@ -50,95 +50,95 @@ __global__ __launch_bounds__(kScoreThreads) __attribute__((amdgpu_waves_per_eu(2
   const int r = lane & 15, q = lane >> 4;
   const int64_t rows = (int64_t)p.ns * p.hkv, items = rows * ((p.max_ctx + kScoreKeys - 1) / kScoreKeys);
   for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-  const int64_t bg = item % rows;
-  const int tile = (int)(item / rows);
-  const int b = (int)(bg / p.hkv), g = (int)(bg - (int64_t)b * p.hkv);
-  const int ctx = min(p.ctx_lens[b], p.max_ctx);
-  const int k0 = tile * kScoreKeys + wave * kWaveChunks * kChunk;  // this wave's first key
-  if (k0 >= ctx) continue;
-  const int pos0 = ctx - p.nq;  // the first query's position
-  const int ncols = p.nq * p.group;
+    const int64_t bg = item % rows;
+    const int tile = (int)(item / rows);
+    const int b = (int)(bg / p.hkv), g = (int)(bg - (int64_t)b * p.hkv);
+    const int ctx = min(p.ctx_lens[b], p.max_ctx);
+    const int k0 = tile * kScoreKeys + wave * kWaveChunks * kChunk;  // this wave's first key
+    if (k0 >= ctx) continue;
+    const int pos0 = ctx - p.nq;  // the first query's position
+    const int ncols = p.nq * p.group;
 
-  u32x4 ka[kWaveChunks][4], kb[kWaveChunks][4];
-  bool held[kWaveChunks];  // whether this lane's keys 8 q .. 8 q + 7 of the chunk are in the pool
-#pragma unroll
-  for (int c = 0; c < kWaveChunks; ++c) {
-    const int key = k0 + c * kChunk;
-    auto page_of = [&](int k) {
-      const int lp = k >> pv.pg_shift;
-      if (k >= ctx) return -1;  // (a page past the context is not read)
-      const int64_t v = pv.table[(int64_t)b * pv.stride + lp];
-      return v >= 0 && v < pv.num_pages ? (int)v : -1;
-    };
-    const int pa = page_of(key), pb = kOnePage ? pa : page_of(key + 16);
-    held[c] = (kOnePage || !(q & 2) ? pa : pb) >= 0;
-    const int page = kOnePage || !(r & 8) ? pa : pb;  // of this lane's K rows
-    const char *base = reinterpret_cast<const char *>(pv.k_pool) +
-                       (((int64_t)max(page, 0) * p.hkv + g) << (pv.pg_shift + kHeadDimShift + 1));
-    uint32_t off;
-    if constexpr (kOnePage) off = ((key & ((1 << pv.pg_shift) - 1)) << (kHeadDimShift + 1)) + lane * 16;
-    else off = (q * 8 + (r & 7)) * 16;
-    constexpr uint32_t slab = kOnePage ? 1024 : 512;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const u32x4 z = {0u, 0u, 0u, 0u};
-      ka[c][t] = page >= 0 ? ldg128(base + off + slab * t) : z;
-      kb[c][t] = page >= 0 ? ldg128(base + off + slab * (t + 4)) : z;
-    }
-  }
-  float w[kWaveChunks][8] = {};  // keys 8 q + i of the chunk, column r's share
-  // column r of a group of 16: its queries' operands and log-sum-exp, loaded a group ahead
-  struct Columns {
-    u32x4 q[4];
-    float lse;
-    int last;  // the last key it sees
-  };
-  auto load_columns = [&](int c0, Columns &x) {
-    const int col = c0 + r;
-    const bool valid = col < ncols;
-    const int qi = valid ? col / p.group : 0;
-    const int64_t row = ((int64_t)b * p.nq + qi) * p.hq + (int64_t)g * p.group + (valid ? col - qi * p.group : 0);
-    x.lse = p.row_lse[row];
-    x.last = valid ? pos0 + qi : -1;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) x.q[t] = ldg128(p.q + row * kHeadDim + 32 * t + 8 * q);
-  };
-  Columns next;
-  load_columns(0, next);
-  for (int c0 = 0; c0 < ncols; c0 += kCols) {
-    const Columns now = next;
-    if (c0 + kCols < ncols) load_columns(c0 + kCols, next);
+    u32x4 ka[kWaveChunks][4], kb[kWaveChunks][4];
+    bool held[kWaveChunks];  // whether this lane's keys 8 q .. 8 q + 7 of the chunk are in the pool
 #pragma unroll
     for (int c = 0; c < kWaveChunks; ++c) {
-      f32x4 sa = {0.f, 0.f, 0.f, 0.f}, sb = sa;
+      const int key = k0 + c * kChunk;
+      auto page_of = [&](int k) {
+        const int lp = k >> pv.pg_shift;
+        if (k >= ctx) return -1;  // (a page past the context is not read)
+        const int64_t v = pv.table[(int64_t)b * pv.stride + lp];
+        return v >= 0 && v < pv.num_pages ? (int)v : -1;
+      };
+      const int pa = page_of(key), pb = kOnePage ? pa : page_of(key + 16);
+      held[c] = (kOnePage || !(q & 2) ? pa : pb) >= 0;
+      const int page = kOnePage || !(r & 8) ? pa : pb;  // of this lane's K rows
+      const char *base = reinterpret_cast<const char *>(pv.k_pool) +
+                         (((int64_t)max(page, 0) * p.hkv + g) << (pv.pg_shift + kHeadDimShift + 1));
+      uint32_t off;
+      if constexpr (kOnePage) off = ((key & ((1 << pv.pg_shift) - 1)) << (kHeadDimShift + 1)) + lane * 16;
+      else off = (q * 8 + (r & 7)) * 16;
+      constexpr uint32_t slab = kOnePage ? 1024 : 512;
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        sa = mfma16x16x32(ka[c][t], now.q[t], sa);
-        sb = mfma16x16x32(kb[c][t], now.q[t], sb);
+        const u32x4 z = {0u, 0u, 0u, 0u};
+        ka[c][t] = page >= 0 ? ldg128(base + off + slab * t) : z;
+        kb[c][t] = page >= 0 ? ldg128(base + off + slab * (t + 4)) : z;
       }
-      const int j0 = k0 + c * kChunk + 8 * q;
+    }
+    float w[kWaveChunks][8] = {};  // keys 8 q + i of the chunk, column r's share
+    // column r of a group of 16: its queries' operands and log-sum-exp, loaded a group ahead
+    struct Columns {
+      u32x4 q[4];
+      float lse;
+      int last;  // the last key it sees
+    };
+    auto load_columns = [&](int c0, Columns &x) {
+      const int col = c0 + r;
+      const bool valid = col < ncols;
+      const int qi = valid ? col / p.group : 0;
+      const int64_t row = ((int64_t)b * p.nq + qi) * p.hq + (int64_t)g * p.group + (valid ? col - qi * p.group : 0);
+      x.lse = p.row_lse[row];
+      x.last = valid ? pos0 + qi : -1;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) x.q[t] = ldg128(p.q + row * kHeadDim + 32 * t + 8 * q);
+    };
+    Columns next;
+    load_columns(0, next);
+    for (int c0 = 0; c0 < ncols; c0 += kCols) {
+      const Columns now = next;
+      if (c0 + kCols < ncols) load_columns(c0 + kCols, next);
+#pragma unroll
+      for (int c = 0; c < kWaveChunks; ++c) {
+        f32x4 sa = {0.f, 0.f, 0.f, 0.f}, sb = sa;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          sa = mfma16x16x32(ka[c][t], now.q[t], sa);
+          sb = mfma16x16x32(kb[c][t], now.q[t], sb);
+        }
+        const int j0 = k0 + c * kChunk + 8 * q;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float s = i < 4 ? sa[i & 3] : sb[i & 3];
+          const float e = fast_exp2(fmaf(s, p.scale_log2, -now.lse));
+          w[c][i] += held[c] && j0 + i <= now.last ? e : 0.f;
+        }
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < kWaveChunks; ++c) {
+      float mine = 0.f;  // lane r of a row takes key 8 q + r (r < 8)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float s = i < 4 ? sa[i & 3] : sb[i & 3];
-        const float e = fast_exp2(fmaf(s, p.scale_log2, -now.lse));
-        w[c][i] += held[c] && j0 + i <= now.last ? e : 0.f;
+        const float t = row_sum16(w[c][i]);
+        mine = r == i ? t : mine;
+      }
+      const int j = k0 + c * kChunk + 8 * q + r;
+      if (r < 8 && j < ctx) {
+        const int64_t at = bg * sp.stride + j;
+        sp.scores_out[at] = (sp.scores_in ? sp.scores_in[at] : 0.f) + mine;
       }
     }
-  }
-#pragma unroll
-  for (int c = 0; c < kWaveChunks; ++c) {
-    float mine = 0.f;  // lane r of a row takes key 8 q + r (r < 8)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float t = row_sum16(w[c][i]);
-      mine = r == i ? t : mine;
-    }
-    const int j = k0 + c * kChunk + 8 * q + r;
-    if (r < 8 && j < ctx) {
-      const int64_t at = bg * sp.stride + j;
-      sp.scores_out[at] = (sp.scores_in ? sp.scores_in[at] : 0.f) + mine;
-    }
-  }
   }
 }
 

@@ -20,15 +20,15 @@
 //           own keys over 8192 shared ones took 23 + 26 us, 41 so.)
 //   merge   the partials of each row
 // Every workgroup finds the plan by itself, in one wave: a kernel for it
-// took 9 us. Batches of more than 64 sequences or 63 groups have that kernel
-// (shared_plan_kernel).
+// took 9 us. Batches of more than 64 sequences or 63 groups (or 2^31 own chunks)
+// have that kernel (shared_plan_kernel).
 // The key tiles of all (group, KV head, 256 columns), in that order, are cut into
 // equal spans, one per prefix workgroup. Where there are few of these column
 // tiles, each is padded to a multiple of a span, so that none crosses from one to
-// the next (a second start took such a workgroup 8 of 37 us). Its two phases (matrix products, softmax
-// with the staging of tiles) alternate between two groups of four waves, one
-// wave of each on a SIMD, as in prefill.hip. Every shared tile is whole and seen
-// by every query, so it needs no masks.
+// the next (a second start took such a workgroup 8 of 37 us). Its two phases
+// (matrix products, softmax with the staging of tiles) alternate between two
+// groups of four waves, one wave of each on a SIMD, as in prefill.hip. Every
+// shared tile is whole and seen by every query, so it needs no masks.
 #include <algorithm>
 #include <type_traits>
 
@@ -900,7 +900,9 @@ hipError_t launch_cg(const SharedParams &p0, hipStream_t stream) {
   SharedParams p = p0;
   DecodeParams &d = p.d;
   d.item_cols = kCGd * kCols;
-  p.small = d.ns <= kWave && p.ng < kWave;
+  const int64_t chunks = (int64_t)d.ns * ((d.max_ctx + kChunk - 1) / kChunk);
+  const int heads = d.hkv * ((d.nq * d.group + d.item_cols - 1) / d.item_cols);
+  p.small = d.ns <= kWave && p.ng < kWave && chunks * heads <= INT32_MAX;  // (its sums are 32-bit)
   hipError_t e = p.small ? hipSuccess : launch_kernel(shared_plan_kernel, dim3(1), dim3(kPlanThreads), stream, p);
   if (e != hipSuccess) return e;
   if ((e = launch_work<kCGd, kMode>(p, stream)) != hipSuccess) return e;

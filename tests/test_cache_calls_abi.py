@@ -39,6 +39,7 @@ def _evict(layer=None, shape=None, src=None, dst=None, scores=FAKE, stride=500, 
     (dict(shape=_shape(d=64)), UNSUPPORTED), (dict(shape=_shape(hq=63)), INVALID), (dict(shape=_shape(pg=48)), UNSUPPORTED),
     (dict(ns=-1), INVALID), (dict(maxc=0), INVALID), (dict(recent=-1), INVALID), (dict(sinks=-1), INVALID),
     (dict(kstride=0), INVALID), (dict(ns=1 << 20), UNSUPPORTED),
+    (dict(maxc=(1 << 30) + 1), UNSUPPORTED), (dict(kstride=(1 << 30) + 1), UNSUPPORTED),
     (dict(stride=499), CAPACITY), (dict(src=_cache(7)), CAPACITY), (dict(dst=_cache(1, 10, FAKE2)), CAPACITY),
     (dict(so=FAKE2, sostride=99), CAPACITY),
     (dict(dst=_cache(8, 10, FAKE)), INVALID), (dict(so=FAKE, sostride=100), INVALID),
@@ -94,6 +95,7 @@ def _scored(layer=None, shape=None, cache=None, q=FAKE, ctx=FAKE, ns=2, nq=1, ma
     (dict(stride=499), CAPACITY), (dict(cache=_cache(7)), CAPACITY), (dict(wsb=1000), CAPACITY),
     (dict(q=None), INVALID), (dict(ctx=None), INVALID), (dict(so=None), INVALID), (dict(out=None), INVALID),
     (dict(ws=None), INVALID),
+    (dict(maxc=(1 << 30) + 1), UNSUPPORTED), (dict(ns=(1 << 19) + 1), UNSUPPORTED),  # 2^25 rows of 64 heads
 ])
 def test_decode_scored_refusals(kw, code):
     assert _scored(**kw) == code
@@ -103,7 +105,7 @@ def test_decode_scored_workspace():
     sh = hswa.Shape(64, 8)
     assert hswa.decode_scored_workspace_bytes(sh, 2, 1, 100) > 0
     assert hswa.decode_scored_workspace_bytes(sh, 2, 1, 5000) > hswa.decode_workspace_bytes(sh, 2, 5000)
-    for a in ((0, 1, 100), (2, 0, 100), (2, 65, 100), (2, 1, 0)):
+    for a in ((0, 1, 100), (2, 0, 100), (2, 65, 100), (2, 1, 0), (2, 1, (1 << 30) + 1)):
         assert hswa.decode_scored_workspace_bytes(sh, *a) == 0
 
 
@@ -134,6 +136,7 @@ def _shared(layer=None, shape=None, cache=None, q=FAKE, ctx=FAKE, ns=400, nq=1, 
     (dict(cu=None), INVALID), (dict(sl=None), INVALID),
     (dict(cache=_cache(7)), CAPACITY), (dict(cache=_cache(pages=0)), INVALID), (dict(wsb=1000), CAPACITY),
     (dict(q=None), INVALID), (dict(ctx=None), INVALID), (dict(out=None), INVALID), (dict(ws=None), INVALID),
+    (dict(ns=(1 << 19) + 1), UNSUPPORTED),  # 2^25 rows of 64 heads
     # without a group, or a tile that could be shared, the refusals of decode_multi
     (dict(ng=0, cu=None, sl=None, q=None), INVALID), (dict(top=63, wsb=0, ws=None), INVALID),
     (dict(ng=0, cache=_cache(7)), CAPACITY), (dict(ng=0, nq=65), INVALID),
@@ -151,6 +154,9 @@ def test_decode_shared_workspace():
         assert hswa.decode_shared_workspace_bytes(sh, ns, 2, 5000, ng, top) == hswa.decode_multi_workspace_bytes(
             sh, ns, 2, 5000)
     assert hswa.decode_shared_workspace_bytes(sh, 19, 2, 5000, 1, 1000) > hswa.decode_multi_workspace_bytes(sh, 19, 2, 5000)
+    # contexts past 2^30 too
+    assert hswa.decode_shared_workspace_bytes(sh, 2, 1, (1 << 30) + 1, 1, 5000000) == hswa.decode_multi_workspace_bytes(
+        sh, 2, 1, (1 << 30) + 1)
     for a in ((0, 1, 100, 0, 0), (2, 0, 100, 1, 64), (2, 65, 100, 1, 64), (2, 1, 0, 1, 64), (2, 1, 100, 3, 64),
               (2, 1, 100, -1, 64), (2, 1, 100, 1, -1)):
         assert hswa.decode_shared_workspace_bytes(sh, *a) == 0
