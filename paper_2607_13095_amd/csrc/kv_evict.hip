@@ -11,7 +11,8 @@
 //
 // Move. Kept keys keep their order, so slot i of the new pages is the i-th kept
 // position; every KV head keeps its own set (a page holds its heads apart). One
-// workgroup per 32 slots of a (sequence, KV head).
+// workgroup per 32 slots of a (sequence, KV head). Where these are no more than
+// the compute units, one kernel does both.
 #include <algorithm>
 
 #include "hswa_common.h"
@@ -29,6 +30,7 @@ constexpr int kCopies = 4;  // of the histogram, for lanes that meet in a bin
 constexpr int kMoveThreads = 256;
 constexpr int kSlots = 32;        // slots of the new pages per workgroup of the move
 constexpr int kMaxMoveGrid = 1 << 20;
+constexpr int kSmallItems = 256;  // a workgroup per compute unit
 
 // What a sequence keeps, by count: its first and last keys and those picked by
 // score out of [sinks, len - recent).
@@ -55,24 +57,19 @@ __device__ __forceinline__ uint32_t score_key(float s) {
 // kPer: scores that a thread holds in registers, 64 positions of a wave apart; 0:
 // any number, read again for each of the five passes, kBatch loads at a time
 // (one at a time a pass over 58K scores took 20 us; 64 held spilled).
-template <int kPer>
-__global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictParams p) {
+struct SelectLds {
+  uint32_t hist[kBins * kCopies];
+  uint32_t wsum[2][kSelectWaves];
+  uint32_t found[3];
+};
+// emit(slot, position, score) for every kept key of row (b, g), by kSelectThreads.
+template <int kPer, typename Emit>
+__device__ __forceinline__ void select_row(const Keep &n, const float *scores, SelectLds &lds, Emit emit) {
   constexpr int kEach = kBins / kSelectThreads;  // bins of a thread
-  __shared__ uint32_t hist[kBins * kCopies];
-  __shared__ uint32_t wsum[2][kSelectWaves];
-  __shared__ uint32_t found[3];
+  auto &hist = lds.hist;
+  auto &wsum = lds.wsum;
+  auto &found = lds.found;
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-  const int b = (int)(blockIdx.x / p.hkv), g = (int)(blockIdx.x - (int64_t)b * p.hkv);
-  const Keep n = keep_of(p, b);
-  if (g == 0 && tid == 0) p.new_lens[b] = n.keep;
-  const int64_t row = (int64_t)b * p.hkv + g;
-  const float *scores = p.scores + row * p.score_stride;
-  int32_t *kept = p.kept + row * p.max_keep;
-  float *out = p.scores_out ? p.scores_out + row * p.out_stride : nullptr;
-  auto emit = [&](int slot, int pos) {
-    kept[slot] = pos;
-    if (out) out[slot] = scores[pos];
-  };
   const int lo = n.sinks, hi = n.len - n.recent;
   // this wave's stretch of the positions that are picked from: groups of 64
   const int groups = (hi - lo + kSelectWaves * kWave - 1) / (kSelectWaves * kWave);
@@ -86,10 +83,10 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictParam
       held[e] = i < w1 ? scores[i] : 0.f;
     }
   }
-  for (int i = tid; i < n.sinks; i += kSelectThreads) emit(i, i);
-  for (int i = tid; i < n.recent; i += kSelectThreads) emit(n.keep - n.recent + i, hi + i);
+  for (int i = tid; i < n.sinks; i += kSelectThreads) emit(i, i, scores[i]);
+  for (int i = tid; i < n.recent; i += kSelectThreads) emit(n.keep - n.recent + i, hi + i, scores[hi + i]);
   if (!choose) {
-    for (int i = tid; i < n.pick; i += kSelectThreads) emit(lo + i, lo + i);
+    for (int i = tid; i < n.pick; i += kSelectThreads) emit(lo + i, lo + i, scores[lo + i]);
     return;
   }
   // f(position, key, whether there is one) for 64 positions of the stretch at a time
@@ -205,13 +202,32 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictParam
     const uint64_t same = __ballot(in && k == top);
     const bool keep = in && (k > top || (k == top && eq + __popcll(same & below) < need));
     const uint64_t mine = __ballot(keep);
-    if (keep) {
-      const int to = (int)slot + __popcll(mine & below);
-      kept[to] = i;
-      if (out) out[to] = score;
-    }
+    if (keep) emit((int)slot + __popcll(mine & below), i, score);
     slot += __popcll(mine);
     eq += __popcll(same);
+  });
+}
+
+// Where a row's kept positions and their scores go.
+struct KeptRow {
+  int32_t *kept;
+  float *scores;
+};
+__device__ __forceinline__ KeptRow kept_row(const EvictParams &p, int64_t row) {
+  return KeptRow{p.kept + row * p.max_keep, p.scores_out ? p.scores_out + row * p.out_stride : nullptr};
+}
+
+template <int kPer>
+__global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictParams p) {
+  __shared__ SelectLds lds;
+  const int b = (int)(blockIdx.x / p.hkv), g = (int)(blockIdx.x - (int64_t)b * p.hkv);
+  const Keep n = keep_of(p, b);
+  if (g == 0 && threadIdx.x == 0) p.new_lens[b] = n.keep;
+  const int64_t row = (int64_t)b * p.hkv + g;
+  const KeptRow out = kept_row(p, row);
+  select_row<kPer>(n, p.scores + row * p.score_stride, lds, [&](int slot, int pos, float score) {
+    out.kept[slot] = pos;
+    if (out.scores) out.scores[slot] = score;
   });
 }
 
@@ -225,23 +241,127 @@ __device__ __forceinline__ int page_of(const PoolView &pv, int b, int j) {
 
 // 32 slots of the new pages. K moves in 16-byte pieces (8 dims of a key). V is
 // stored with a block's keys side by side, so a kept key is 2 bytes here and
-// there: each wave takes 32 dims, loads whole rows of the blocks that hold kept
-// keys (kStageBlocks, a power of two, at a time, in LDS) and picks from them the
-// 16 slots of a lane's dim. kB: keys of a block (16 for 16-key pages, else 32).
+// there: each of kVWaves waves takes its share of the dims, loads whole rows of
+// the blocks that hold kept keys (kStageBlocks, a power of two, at a time, in
+// LDS) and picks from them the slots of each lane, of one dim. kB: keys of a block
+// (16 for 16-key pages, else 32). kKWaves: waves that move K; V starts with wave
+// kVFirst.
+template <int kB, int kStageBlocks, int kKWaves, int kVFirst, int kVWaves>
+struct Move {
+  static constexpr int kDims = kHeadDim / kVWaves;      // dims of a wave
+  static constexpr int kRow = 2 * kB / 16;              // 16-byte pieces of a block's row
+  static constexpr int kPad = kRow + 1;                 // and of a row in LDS
+  static constexpr int kLoads = kDims * kRow / kWave;   // pieces of a block for a lane
+  static constexpr int kLanes = kWave / kDims;          // lanes of a dim
+  static constexpr int kPick = kSlots / kLanes;         // slots of a lane
+  static_assert(kLoads * kWave == kDims * kRow && kPick % 8 == 0, "whole loads, whole 16-byte stores");
+  struct Lds {
+    u32x4 stage[kVWaves][kStageBlocks][kDims * kPad];
+    int page[kSlots], off[kSlots];  // source page (-1: none) and offset of each slot
+    int block[kSlots];              // its block, numbered among those of this workgroup
+    int first[kSlots + 1];          // first slot of each block
+    int to[kSlots];                 // page of each slot (-1: none)
+    int blocks, count;
+  };
+
+  // By one wave: lane l < count keeps position j, of page `from`, for a slot on page `to`.
+  __device__ static __forceinline__ void plan(Lds &s, int pgm, int count, int j, int from, int to) {
+    const int lane = threadIdx.x & (kWave - 1);
+    const bool in = lane < count;
+    const int before = __shfl_up(j, 1, kWave);
+    const uint64_t starts = __ballot(in && (lane == 0 || j / kB != before / kB));
+    if (lane < kSlots) {
+      s.to[lane] = in ? to : -1;
+      s.page[lane] = in ? from : -1;
+      s.off[lane] = j & pgm;
+      const int blk = __popcll(starts & (((uint64_t)2 << lane) - 1)) - 1;
+      s.block[lane] = blk;
+      if ((starts >> lane) & 1) s.first[blk] = lane;
+    }
+    if (lane == 0) {
+      s.blocks = __popcll(starts);
+      s.first[__popcll(starts)] = count;
+      s.count = count;
+    }
+  }
+
+  // The n slots from s0 on of KV head g, as planned.
+  __device__ static __forceinline__ void run(const EvictParams &p, Lds &s, int g, int s0, int n) {
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int pgm = (1 << p.src.pg_shift) - 1;
+    const u32x4 z = {0u, 0u, 0u, 0u};
+    if (wave < kKWaves) {
+      // K: pieces in the order of the new block, so that stores are whole runs
+      constexpr int rb = kB == 32 ? 4 : 3;  // log2 of the rows of a half block
+#pragma unroll
+      for (int y = 0; y < kSlots * 16 / (kKWaves * kWave); ++y) {
+        const int x = tid + y * kKWaves * kWave;
+        const int r = x & ((1 << rb) - 1), piece = (x >> rb) & 3, slab = (x >> (rb + 2)) & 3, half = (x >> (rb + 4)) & 1;
+        const int i = ((x >> (rb + 5)) << (rb + 1)) + 8 * (r >> 2) + 4 * half + (r & 3);
+        const int d = 32 * slab + 8 * piece;
+        const int to = s.to[i];
+        if (to < 0) continue;
+        const u32x4 v = s.page[i] >= 0 ? ldg128(p.src.k_pool + k_offset(p.src, s.page[i], p.hkv, g, s.off[i], d)) : z;
+        stg128(p.dst.k_pool + k_offset(p.dst, to, p.hkv, g, (s0 + i) & pgm, d), v);
+      }
+    }
+    if (wave < kVFirst || wave >= kVFirst + kVWaves) return;
+    // V: lane = (dim, kPick slots)
+    const int vw = wave - kVFirst, d = vw * kDims + lane / kLanes, i0 = kPick * (lane & (kLanes - 1));
+    uint32_t val[kPick / 2] = {};  // two slots each
+    const int blocks = s.blocks;
+    for (int b0 = 0; b0 < blocks; b0 += kStageBlocks) {
+      u32x4 ld[kStageBlocks][kLoads];
+#pragma unroll
+      for (int k = 0; k < kStageBlocks; ++k) {
+        const int first = s.first[min(b0 + k, blocks - 1)];
+        const int page = s.page[first];
+        const uint16_t *src = p.src.v_pool + v_offset(p.src, max(page, 0), p.hkv, g, s.off[first] & ~(kB - 1), vw * kDims);
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l)
+          ld[k][l] = b0 + k < blocks && page >= 0 ? ldg128(src + (l * kWave + lane) * 8) : z;
+      }
+      __builtin_amdgcn_wave_barrier();  // (the picks from the blocks before are done)
+#pragma unroll
+      for (int k = 0; k < kStageBlocks; ++k)
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l) {
+          const int x = l * kWave + lane;
+          s.stage[vw][k][x / kRow * kPad + x % kRow] = ld[k][l];
+        }
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int e = 0; e < kPick; ++e) {
+        const int blk = s.block[i0 + e] - b0;
+        const uint16_t *rowp =
+            reinterpret_cast<const uint16_t *>(&s.stage[vw][blk & (kStageBlocks - 1)][lane / kLanes * kPad]);
+        const uint32_t v = rowp[s.off[i0 + e] & (kB - 1)];
+        if (blk >= 0 && blk < kStageBlocks) val[e >> 1] |= v << (16 * (e & 1));
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+    const int to = s.to[i0];
+    if (to < 0) return;
+    uint16_t *dst = p.dst.v_pool + v_offset(p.dst, to, p.hkv, g, (s0 + i0) & pgm, d);
+#pragma unroll
+    for (int h = 0; h < kPick / 8; ++h) {
+      if (i0 + 8 * h + 8 <= n) {
+        stg128(dst + 8 * h, u32x4{val[4 * h], val[4 * h + 1], val[4 * h + 2], val[4 * h + 3]});
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (i0 + 8 * h + e < n) dst[8 * h + e] = (uint16_t)(val[4 * h + (e >> 1)] >> (16 * (e & 1)));
+      }
+    }
+  }
+};
+
 template <int kB, int kStageBlocks>
 __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictParams p) {
-  constexpr int kDims = kHeadDim / (kMoveThreads / kWave);  // dims of a wave
-  constexpr int kRow = 2 * kB / 16;                         // 16-byte pieces of a block's row
-  constexpr int kPad = kRow + 1;                            // and of a row in LDS
-  constexpr int kLoads = kDims * kRow / kWave;              // pieces of a block for a lane
-  static_assert(kDims * 2 == kWave, "two lanes a dim");
-  __shared__ u32x4 stage[kMoveThreads / kWave][kStageBlocks][kDims * kPad];
-  __shared__ int s_page[kSlots], s_off[kSlots];  // source page (-1: none) and offset of each slot
-  __shared__ int s_block[kSlots];                // its block, numbered among those of this workgroup
-  __shared__ int s_first[kSlots + 1];            // first slot of each block
-  __shared__ int s_to[kSlots];                   // page of each slot (-1: none)
-  __shared__ int s_blocks, s_count;
-  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  constexpr int kMoveWaves = kMoveThreads / kWave;
+  using M = Move<kB, kStageBlocks, kMoveWaves, 0, kMoveWaves>;
+  __shared__ typename M::Lds s;
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int64_t chunks = (p.max_keep + kSlots - 1) / kSlots, total = chunks * p.ns * p.hkv;
   const int pgm = (1 << p.src.pg_shift) - 1;
   for (int64_t item = blockIdx.x; item < total; item += gridDim.x) {
@@ -257,103 +377,76 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictParams p)
       int j = at < p.max_keep ? p.kept[row * p.max_keep + at] : 0;
       const int to = page_of(p.dst, b, at);
       const int count = min(len - s0, kSlots);
-      const bool in = lane < count;
-      j = in ? j : 0;
-      const int before = __shfl_up(j, 1, kWave);
-      const uint64_t starts = __ballot(in && (lane == 0 || j / kB != before / kB));
-      if (lane < kSlots) {
-        s_to[lane] = in ? to : -1;
-        s_page[lane] = in ? page_of(p.src, b, j) : -1;
-        s_off[lane] = j & pgm;
-        const int blk = __popcll(starts & (((uint64_t)2 << lane) - 1)) - 1;
-        s_block[lane] = blk;
-        if ((starts >> lane) & 1) s_first[blk] = lane;
-      }
-      if (lane == 0) {
-        s_blocks = __popcll(starts);
-        s_first[__popcll(starts)] = count;
-        s_count = count;
-      }
+      j = lane < count ? j : 0;
+      M::plan(s, pgm, count, j, lane < count ? page_of(p.src, b, j) : -1, to);
     }
     __syncthreads();
-    const int n = s_count;  // slots of this workgroup
-    if (n <= 0) continue;
-    const u32x4 z = {0u, 0u, 0u, 0u};
-    // K: pieces in the order of the new block, so that stores are whole runs
-    constexpr int rb = kB == 32 ? 4 : 3;  // log2 of the rows of a half block
-#pragma unroll
-    for (int y = 0; y < kSlots * 16 / kMoveThreads; ++y) {
-      const int x = tid + y * kMoveThreads;
-      const int r = x & ((1 << rb) - 1), piece = (x >> rb) & 3, slab = (x >> (rb + 2)) & 3, half = (x >> (rb + 4)) & 1;
-      const int i = ((x >> (rb + 5)) << (rb + 1)) + 8 * (r >> 2) + 4 * half + (r & 3);
-      const int d = 32 * slab + 8 * piece;
-      const int to = s_to[i];
-      if (to < 0) continue;
-      const u32x4 v = s_page[i] >= 0 ? ldg128(p.src.k_pool + k_offset(p.src, s_page[i], p.hkv, g, s_off[i], d)) : z;
-      stg128(p.dst.k_pool + k_offset(p.dst, to, p.hkv, g, (s0 + i) & pgm, d), v);
-    }
-    // V: lane = (dim, 16 slots)
-    const int d = wave * kDims + (lane >> 1), i0 = 16 * (lane & 1);
-    uint32_t val[8] = {};  // two slots each
-    const int blocks = s_blocks;
-    for (int b0 = 0; b0 < blocks; b0 += kStageBlocks) {
-      u32x4 ld[kStageBlocks][kLoads];
-#pragma unroll
-      for (int k = 0; k < kStageBlocks; ++k) {
-        const int first = s_first[min(b0 + k, blocks - 1)];
-        const int page = s_page[first];
-        const uint16_t *src = p.src.v_pool + v_offset(p.src, max(page, 0), p.hkv, g, s_off[first] & ~(kB - 1), wave * kDims);
-#pragma unroll
-        for (int l = 0; l < kLoads; ++l)
-          ld[k][l] = b0 + k < blocks && page >= 0 ? ldg128(src + (l * kWave + lane) * 8) : z;
-      }
-      __builtin_amdgcn_wave_barrier();  // (the picks from the blocks before are done)
-#pragma unroll
-      for (int k = 0; k < kStageBlocks; ++k)
-#pragma unroll
-        for (int l = 0; l < kLoads; ++l) {
-          const int x = l * kWave + lane;
-          stage[wave][k][x / kRow * kPad + x % kRow] = ld[k][l];
-        }
-      __builtin_amdgcn_wave_barrier();
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int blk = s_block[i0 + e] - b0;
-        const uint16_t *rowp =
-            reinterpret_cast<const uint16_t *>(&stage[wave][blk & (kStageBlocks - 1)][(lane >> 1) * kPad]);
-        const uint32_t v = rowp[s_off[i0 + e] & (kB - 1)];
-        if (blk >= 0 && blk < kStageBlocks) val[e >> 1] |= v << (16 * (e & 1));
-      }
-      __builtin_amdgcn_wave_barrier();
-    }
-    const int to = s_to[i0];
-    if (to >= 0) {
-      uint16_t *dst = p.dst.v_pool + v_offset(p.dst, to, p.hkv, g, (s0 + i0) & pgm, d);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        if (i0 + 8 * h + 8 <= n) {
-          stg128(dst + 8 * h, u32x4{val[4 * h], val[4 * h + 1], val[4 * h + 2], val[4 * h + 3]});
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (i0 + 8 * h + e < n) dst[8 * h + e] = (uint16_t)(val[4 * h + (e >> 1)] >> (16 * (e & 1)));
-        }
-      }
-    }
+    if (s.count <= 0) continue;
+    M::run(p, s, g, s0, s.count);
   }
+}
+
+// Both for few slots: every workgroup selects for its row by itself and moves
+// its 32 slots, half of the waves K and half V; the second launch and the way of
+// the positions through memory are saved. us a call, one kernel and two (8 KV
+// heads): 1 x 1000 to 300 11.1 and 14.2, 1 x 4100 to 1024 15.1 and 17.5, 1 x 16000
+// to 1000 27.2 and 30.8, 32 x 300 to 30 15.9 and 19.9; with more workgroups than
+// compute units (two in LDS do not fit one) 2 x 4000 to 1000 26.4 and 21.2.
+// kPer as above, 1 or more.
+template <int kPer, int kB>
+__global__ __launch_bounds__(kSelectThreads) void evict_small_kernel(EvictParams p) {
+  using M = Move<kB, 8, kSelectWaves / 2, kSelectWaves / 2, kB == 32 ? 8 : 4>;
+  __shared__ SelectLds lds;
+  __shared__ typename M::Lds s;
+  __shared__ int s_kept[kSlots];
+  __shared__ int s_pages[kPer * kSelectThreads / kB];  // the row of the source's table
+  const int tid = threadIdx.x, lane = tid & (kWave - 1);
+  const int chunks = (p.max_keep + kSlots - 1) / kSlots;
+  const int row = (int)blockIdx.x / chunks, s0 = ((int)blockIdx.x - row * chunks) * kSlots;
+  const int b = row / p.hkv, g = row - b * p.hkv;
+  const Keep n = keep_of(p, b);
+  if (g == 0 && s0 == 0 && tid == 0) p.new_lens[b] = n.keep;
+  const int count = min(n.keep - s0, kSlots);
+  if (count <= 0) return;
+  const int to = tid < kSlots ? page_of(p.dst, b, s0 + tid) : -1;
+  const int pages = (n.len + (1 << p.src.pg_shift) - 1) >> p.src.pg_shift;
+  for (int i = tid; i < pages; i += kSelectThreads) s_pages[i] = page_of(p.src, b, i << p.src.pg_shift);
+  const KeptRow out = kept_row(p, row);
+  select_row<kPer>(n, p.scores + (int64_t)row * p.score_stride, lds, [&](int slot, int pos, float score) {
+    if (slot < s0 || slot >= s0 + kSlots) return;
+    s_kept[slot - s0] = pos;
+    out.kept[slot] = pos;
+    if (out.scores) out.scores[slot] = score;
+  });
+  __syncthreads();
+  if (tid < kWave) {
+    const int j = lane < count ? s_kept[lane] : 0;
+    M::plan(s, (1 << p.src.pg_shift) - 1, count, j, s_pages[j >> p.src.pg_shift], to);
+  }
+  __syncthreads();
+  M::run(p, s, g, s0, count);
 }
 
 }  // namespace
 
 hipError_t launch_kv_evict(const EvictParams &p, hipStream_t stream) {
   const dim3 rows((unsigned)(p.ns * p.hkv)), threads(kSelectThreads);
+  const int64_t items = (int64_t)((p.max_keep + kSlots - 1) / kSlots) * p.ns * p.hkv;
   // scores in registers as far as they fit
+  if (items <= kSmallItems && p.max_ctx <= 16 * kSelectThreads) {
+    const dim3 grid((unsigned)items);
+    const bool few = p.max_ctx <= 4 * kSelectThreads;
+    if (p.src.vb_shift == 4)
+      return few ? launch_kernel(evict_small_kernel<4, 16>, grid, threads, stream, p)
+                 : launch_kernel(evict_small_kernel<16, 16>, grid, threads, stream, p);
+    return few ? launch_kernel(evict_small_kernel<4, 32>, grid, threads, stream, p)
+               : launch_kernel(evict_small_kernel<16, 32>, grid, threads, stream, p);
+  }
   hipError_t e;
   if (p.max_ctx <= 4 * kSelectThreads) e = launch_kernel(evict_select_kernel<4>, rows, threads, stream, p);
   else if (p.max_ctx <= 16 * kSelectThreads) e = launch_kernel(evict_select_kernel<16>, rows, threads, stream, p);
   else e = launch_kernel(evict_select_kernel<0>, rows, threads, stream, p);
   if (e != hipSuccess) return e;
-  const int64_t items = (int64_t)((p.max_keep + kSlots - 1) / kSlots) * p.ns * p.hkv;
   const dim3 grid((unsigned)std::min<int64_t>(items, kMaxMoveGrid)), block(kMoveThreads);
   // With a workgroup per compute unit or fewer, more blocks at a time save waits
   // (1 x 4K to 1024, 8 KV heads: 9.7 and 8.5 us); with more of them, four leave
