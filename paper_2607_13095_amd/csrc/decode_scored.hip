@@ -25,8 +25,13 @@ namespace {
 constexpr int kScoreThreads = kMergeThreads;
 constexpr int kKeptKeys = 4 * kScoreThreads;  // keys of a workgroup, from kept scores
 constexpr int kMaxScoreGrid = 1 << 20;
-constexpr int kWaveChunks = 4;  // 32-key chunks a wave holds at once
-constexpr int kScoreKeys = kScoreThreads / kWave * kWaveChunks * kChunk;  // keys of a workgroup
+constexpr int score_keys(int wave_chunks) { return kScoreThreads / kWave * wave_chunks * kChunk; }  // of a workgroup
+// Below this many workgroups of 512 keys (1.5 a compute unit) they take 128 each. us
+// a call with 128 and 512, 64 / 8 heads: 1 x 1000, 4 queries 24.0 and 26.1; 1 x
+// 4000, 16 queries 30.6 and 36.4; 8 / 1, 24 x 300 - 6000, 4 queries 32.2 and 33.6;
+// with more, 32 / 8, 4 x 3000 - 9000, 16 queries 53.9 and 46.5 (each reads all of
+// the queries).
+constexpr int kFewItems = 384;
 
 // Sum over the 16 lanes of a row.
 __device__ __forceinline__ float row_sum16(float x) {
@@ -40,10 +45,12 @@ __device__ __forceinline__ float row_sum16(float x) {
   return x;
 }
 
-// Weights of 512 keys of a (sequence, KV head), 128 a wave. kOnePage: a
-// 32-key chunk lies in one page.
-template <bool kOnePage>
-__global__ __launch_bounds__(kScoreThreads) __attribute__((amdgpu_waves_per_eu(2))) void score_kernel(ScoredParams sp) {
+// Weights of the keys of a (sequence, KV head), kWaveChunks 32-key chunks a wave.
+// kOnePage: a chunk lies in one page.
+template <bool kOnePage, int kWaveChunks>
+__global__ __launch_bounds__(kScoreThreads) __attribute__((amdgpu_waves_per_eu(kWaveChunks == 1 ? 4 : 2)))
+void score_kernel(ScoredParams sp) {
+  constexpr int kScoreKeys = score_keys(kWaveChunks);
   const DecodeParams &p = sp.s.d;
   const PoolView &pv = p.pool;
   const int lane = threadIdx.x & (kWave - 1), wave = uni((int)(threadIdx.x / kWave));
@@ -244,6 +251,16 @@ hipError_t launch_kept(const ScoredParams &p0, hipStream_t stream) {
               : launch_kernel(scored_finish_kernel<1>, both, threads, stream, sp);
 }
 
+template <int kWaveChunks>
+hipError_t launch_scores(const ScoredParams &p, hipStream_t stream) {
+  const DecodeParams &d = p.s.d;
+  constexpr int keys = score_keys(kWaveChunks);
+  const int64_t items = (int64_t)d.ns * d.hkv * ((d.max_ctx + keys - 1) / keys);
+  const dim3 grid((unsigned)std::min<int64_t>(items, kMaxScoreGrid)), threads(kScoreThreads);
+  return d.pool.pg_shift >= 5 ? launch_kernel(score_kernel<true, kWaveChunks>, grid, threads, stream, p)
+                              : launch_kernel(score_kernel<false, kWaveChunks>, grid, threads, stream, p);
+}
+
 }  // namespace
 
 hipError_t launch_decode_scored(const ScoredParams &p, hipStream_t stream) {
@@ -251,10 +268,8 @@ hipError_t launch_decode_scored(const ScoredParams &p, hipStream_t stream) {
   if (d.nq * d.group <= kKeepColumns) return launch_kept(p, stream);
   const hipError_t e = launch_decode_shared_scored(p.s, stream);
   if (e != hipSuccess) return e;
-  const int64_t items = (int64_t)d.ns * d.hkv * ((d.max_ctx + kScoreKeys - 1) / kScoreKeys);
-  const dim3 grid((unsigned)std::min<int64_t>(items, kMaxScoreGrid)), threads(kScoreThreads);
-  return d.pool.pg_shift >= 5 ? launch_kernel(score_kernel<true>, grid, threads, stream, p)
-                              : launch_kernel(score_kernel<false>, grid, threads, stream, p);
+  const int64_t items = (int64_t)d.ns * d.hkv * ((d.max_ctx + score_keys(4) - 1) / score_keys(4));
+  return items < kFewItems ? launch_scores<1>(p, stream) : launch_scores<4>(p, stream);
 }
 
 }  // namespace hswa
