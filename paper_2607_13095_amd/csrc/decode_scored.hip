@@ -16,6 +16,7 @@
 //     matrix cores. (16 queries, 32 / 8 heads, 4 x 3000 - 9000, PG 16: 41 us by
 //     the split decode, 27 so.)
 #include <algorithm>
+#include <type_traits>
 
 #include "decode_kernels.h"
 
@@ -105,33 +106,39 @@ void score_kernel(ScoredParams sp) {
       const bool valid = col < ncols;
       const int qi = valid ? col / p.group : 0;
       const int64_t row = ((int64_t)b * p.nq + qi) * p.hq + (int64_t)g * p.group + (valid ? col - qi * p.group : 0);
-      x.lse = p.row_lse[row];
-      x.last = valid ? pos0 + qi : -1;
+      x.lse = valid ? p.row_lse[row] : INFINITY;  // (weight 0)
+      x.last = pos0 + qi;
 #pragma unroll
       for (int t = 0; t < 4; ++t) x.q[t] = ldg128(p.q + row * kHeadDim + 32 * t + 8 * q);
     };
     Columns next;
     load_columns(0, next);
-    for (int c0 = 0; c0 < ncols; c0 += kCols) {
-      const Columns now = next;
-      if (c0 + kCols < ncols) load_columns(c0 + kCols, next);
+    // kMasked: some column does not see all of the wave's keys
+    auto columns = [&](auto masked) __attribute__((always_inline)) {
+      constexpr bool kMasked = decltype(masked)::value;
+      for (int c0 = 0; c0 < ncols; c0 += kCols) {
+        const Columns now = next;
+        if (c0 + kCols < ncols) load_columns(c0 + kCols, next);
 #pragma unroll
-      for (int c = 0; c < kWaveChunks; ++c) {
-        f32x4 sa = {0.f, 0.f, 0.f, 0.f}, sb = sa;
+        for (int c = 0; c < kWaveChunks; ++c) {
+          f32x4 sa = {0.f, 0.f, 0.f, 0.f}, sb = sa;
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          sa = mfma16x16x32(ka[c][t], now.q[t], sa);
-          sb = mfma16x16x32(kb[c][t], now.q[t], sb);
-        }
-        const int j0 = k0 + c * kChunk + 8 * q;
+          for (int t = 0; t < 4; ++t) {
+            sa = mfma16x16x32(ka[c][t], now.q[t], sa);
+            sb = mfma16x16x32(kb[c][t], now.q[t], sb);
+          }
+          const int j0 = k0 + c * kChunk + 8 * q;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float s = i < 4 ? sa[i & 3] : sb[i & 3];
-          const float e = fast_exp2(fmaf(s, p.scale_log2, -now.lse));
-          w[c][i] += held[c] && j0 + i <= now.last ? e : 0.f;
+          for (int i = 0; i < 8; ++i) {
+            const float s = i < 4 ? sa[i & 3] : sb[i & 3];
+            const float e = fast_exp2(fmaf(s, p.scale_log2, -now.lse));
+            w[c][i] += !kMasked || j0 + i <= now.last ? e : 0.f;
+          }
         }
       }
-    }
+    };
+    if (k0 + kWaveChunks * kChunk - 1 <= pos0) columns(std::false_type{});
+    else columns(std::true_type{});
 #pragma unroll
     for (int c = 0; c < kWaveChunks; ++c) {
       float mine = 0.f;  // lane r of a row takes key 8 q + r (r < 8)
@@ -140,6 +147,7 @@ void score_kernel(ScoredParams sp) {
         const float t = row_sum16(w[c][i]);
         mine = r == i ? t : mine;
       }
+      if (!held[c]) mine = 0.f;
       const int j = k0 + c * kChunk + 8 * q + r;
       if (r < 8 && j < ctx) {
         const int64_t at = bg * sp.stride + j;
