@@ -472,9 +472,9 @@ __device__ __forceinline__ void decode_waves(const DecodeParams &p, [[maybe_unus
           }
           if constexpr (kMode == kKept) {
             if (colv[cg]) {
-              f32x4 *dst = s_keep[wid] + kept * ncols * 8 + (16 * cg + r) * 4 + q;
+              f32x4 *dst = s_keep[wid] + (kept * ncols + 16 * cg + r) * 8 + 2 * q;
               dst[0] = f32x4{s[0], s[1], s[2], s[3]} * c2;
-              dst[4 * ncols] = f32x4{s[4], s[5], s[6], s[7]} * c2;
+              dst[1] = f32x4{s[4], s[5], s[6], s[7]} * c2;
             }
           }
           const float lmax = max8(s) * c2;

@@ -216,13 +216,12 @@ __global__ __launch_bounds__(kScoreThreads) void scored_finish_kernel(ScoredPara
     __syncthreads();
     const int j = k0 + 4 * tid;
     if (j < ctx) {
-      const int o = (j & (kChunk - 1)) >> 2;  // (see hswa_launch.h for the order)
       const f32x4 *src = reinterpret_cast<const f32x4 *>(p.ws_s) + (bg * p.max_chunks + (j >> 5)) * ncols * 8 +
-                         (o & 1) * 4 * ncols + (o >> 1);
+                         ((j & (kChunk - 1)) >> 2);
       f32x4 w = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
       for (int c = 0; c < ncols; ++c) {
-        const f32x4 s = src[4 * c];
+        const f32x4 s = src[8 * c];
         const float l = s_lse[c];
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] += fast_exp2(s[i] - l);

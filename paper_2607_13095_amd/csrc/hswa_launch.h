@@ -74,8 +74,7 @@ struct DecodeParams {
   // stores the token (k_new / v_new) in its slot and takes its key from them
   int32_t split_append;
   float *row_lse;             // scored decode: [ns * nq * Hq], the rows' log2 sum-exps
-  // or all scores in exp2 units, [ns][Hkv][max_chunks][2][nq * group][4][4]: key k of a 32-key
-  // chunk at half k / 4 % 2, place k / 8, element k % 4
+  // or all scores in exp2 units, [ns][Hkv][max_chunks][nq * group][32]
   float *ws_s;
   int64_t max_chunks;         // 32-key chunks of max_ctx
   const int32_t *start;       // suffix decode: [ns], first key (a multiple of 32) of each sequence
