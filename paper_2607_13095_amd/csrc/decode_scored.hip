@@ -175,6 +175,9 @@ __global__ __launch_bounds__(kScoreThreads) void scored_finish_kernel(ScoredPara
   total = uni64(total) * p.hkv;
   const int64_t per = max((int64_t)(p.split_len / kChunk), (total + p.span_waves - 1) / p.span_waves);
   const int64_t rows = (int64_t)p.ns * p.hkv, items = rows * ((p.max_ctx + kKeptKeys - 1) / kKeptKeys);
+  // whether four keys' scores are one 16-byte access in every row
+  const bool aligned = ((reinterpret_cast<uintptr_t>(sp.scores_in) | reinterpret_cast<uintptr_t>(sp.scores_out) |
+                         (uintptr_t)(sp.stride * sizeof(float))) & 15) == 0;
   const int64_t step = (int64_t)gridDim.x - sp.merge_blocks;
   for (int64_t item = (int64_t)blockIdx.x - sp.merge_blocks; item < items; item += step) {
     const int64_t bg = item % rows;
@@ -182,6 +185,18 @@ __global__ __launch_bounds__(kScoreThreads) void scored_finish_kernel(ScoredPara
     const int ctx = min(p.ctx_lens[b], p.max_ctx);
     const int k0 = (int)(item / rows) * kKeptKeys;
     if (k0 >= ctx) continue;  // (the same for every thread)
+    const int j = k0 + 4 * tid;
+    const int64_t at = bg * sp.stride + j;
+    f32x4 old = {0.f, 0.f, 0.f, 0.f};  // (its loads go out before the others)
+    if (sp.scores_in) {
+      if (aligned && j + 3 < ctx) {
+        old = *reinterpret_cast<const f32x4 *>(sp.scores_in + at);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (j + i < ctx) old[i] = sp.scores_in[at + i];
+      }
+    }
     int64_t before = 0;
     for (int s0 = 0; s0 < b; s0 += kWave) before += wave_sum64(s0 + lane < b ? seq_chunks(p, s0 + lane) : 0);
     const int nch = (ctx + kChunk - 1) / kChunk;
@@ -214,7 +229,6 @@ __global__ __launch_bounds__(kScoreThreads) void scored_finish_kernel(ScoredPara
       if (lane == 0 && c < ncols) s_lse[c] = mx == -INFINITY ? INFINITY : mx + __log2f(sum);
     }
     __syncthreads();
-    const int j = k0 + 4 * tid;
     if (j < ctx) {
       const f32x4 *src = reinterpret_cast<const f32x4 *>(p.ws_s) + (bg * p.max_chunks + (j >> 5)) * ncols * 8 +
                          ((j & (kChunk - 1)) >> 2);
@@ -226,10 +240,13 @@ __global__ __launch_bounds__(kScoreThreads) void scored_finish_kernel(ScoredPara
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] += fast_exp2(s[i] - l);
       }
-      const int64_t at = bg * sp.stride + j;
+      if (aligned && j + 3 < ctx) {
+        *reinterpret_cast<f32x4 *>(sp.scores_out + at) = old + w;
+      } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (j + i < ctx) sp.scores_out[at + i] = (sp.scores_in ? sp.scores_in[at + i] : 0.f) + w[i];
+        for (int i = 0; i < 4; ++i)
+          if (j + i < ctx) sp.scores_out[at + i] = old[i] + w[i];
+      }
     }
   }
 }

@@ -188,3 +188,23 @@ def test_decode_scored_captured(gpu_lib):
         torch.cuda.synchronize()
         assert torch.equal(want, s.scores) and torch.equal(rows.view(torch.int16), s.out.view(torch.int16))
         s.run()
+
+
+@pytest.mark.parametrize("stride", [1204, 1201])
+def test_decode_scored_unaligned_scores(gpu_lib, stride):
+    """Score tensors at every address that fp32 has, in place too: the same bits."""
+    s = Scored([1201, 3, 642], 1, 16, 2, 32, (1409,), stride=stride)
+    s.run()
+    s.check(what="aligned")
+    want, n = s.scores.clone(), s.scores.numel()
+    for off in (1, 2, 3):
+        buf = torch.full((n + 8,), -7.0, device="cuda")
+        s.scores = buf[off:off + n].view(s.start.shape)
+        s.run()
+        assert torch.equal(s.scores, want), off
+        s.scores.copy_(s.start)
+        s.run(scores_in=s.scores)
+        for b, c in enumerate(s.lens):
+            assert torch.equal(s.scores[b, :, :c], want[b, :, :c]), off
+            assert torch.equal(s.scores[b, :, c:], s.start[b, :, c:]), off
+        assert bool((buf[:off] == -7.0).all()) and bool((buf[off + n:] == -7.0).all())
