@@ -26,6 +26,7 @@ constexpr int kSelectWaves = kSelectThreads / kWave;
 constexpr int kDigit = 11;  // bits of a digit: three passes over 32-bit scores
 constexpr int kBins = 1 << kDigit;
 constexpr int kBatch = 16;
+constexpr int kListed = 512;  // keys of a wave's list
 constexpr int kCopies = 4;  // of the histogram, for lanes that meet in a bin
 constexpr int kMoveThreads = 256;
 constexpr int kSlots = 32;        // slots of the new pages per workgroup of the move
@@ -55,16 +56,23 @@ __device__ __forceinline__ uint32_t score_key(float s) {
 }
 
 // kPer: scores that a thread holds in registers, 64 positions of a wave apart; 0:
-// any number, read again for each of the five passes, kBatch loads at a time
-// (one at a time a pass over 58K scores took 20 us; 64 held spilled).
+// any number, read again for each pass, kBatch loads at a time (one at a time a
+// pass over 58K scores took 20 us; 64 held spilled). The second pass lists the keys
+// that share the first digit sought (a twentieth of them, if the scores spread over
+// some orders of magnitude), for the third digit and the counts: three passes
+// instead of five, unless a wave's list is too short (8 x 58K, 8 KV heads: 54 us of
+// selection and 47; 2 x 130K to 2000: 164 us a call and 141).
+template <int kPer>
 struct SelectLds {
   uint32_t hist[kBins * kCopies];
   uint32_t wsum[2][kSelectWaves];
   uint32_t found[3];
+  uint32_t over;                                              // (kPer 0) whether a wave's list is too short
+  uint32_t list[kSelectWaves][kPer == 0 ? kListed : 1];       // keys of the first digit sought, in order
 };
 // emit(slot, position, score) for every kept key of row (b, g), by kSelectThreads.
 template <int kPer, typename Emit>
-__device__ __forceinline__ void select_row(const Keep &n, const float *scores, SelectLds &lds, Emit emit) {
+__device__ __forceinline__ void select_row(const Keep &n, const float *scores, SelectLds<kPer> &lds, Emit emit) {
   constexpr int kEach = kBins / kSelectThreads;  // bins of a thread
   auto &hist = lds.hist;
   auto &wsum = lds.wsum;
@@ -133,14 +141,40 @@ __device__ __forceinline__ void select_row(const Keep &n, const float *scores, S
   // the keys that share `top` the `need` highest stay.
   uint32_t top = 0, known = 0, need = n.pick;
   bool ties = true;  // whether only some of the keys equal to `top` stay
+  uint32_t higher = 0;  // (kPer 0) this wave's keys of a higher first digit
+  int listed = 0;       // and those of its list
+  if (tid == 0) lds.over = 0;
 #pragma unroll 1
   for (int shift = 32 - kDigit;; shift = max(shift - kDigit, 0)) {
     const uint32_t digit = shift == 0 ? (1u << (32 - 2 * kDigit)) - 1 : kBins - 1;
     for (int i = tid; i < kBins * kCopies; i += kSelectThreads) hist[i] = 0;
     __syncthreads();
-    each([&](int, uint32_t k, float, bool in) {
-      if (in && (k & known) == top) atomicAdd(&hist[((k >> shift) & digit) * kCopies + (lane & (kCopies - 1))], 1u);
-    });
+    auto count_digit = [&](uint32_t k) {
+      atomicAdd(&hist[((k >> shift) & digit) * kCopies + (lane & (kCopies - 1))], 1u);
+    };
+    if (kPer == 0 && shift == 32 - 2 * kDigit) {
+      each([&](int, uint32_t k, float, bool in) {
+        const uint64_t same = __ballot(in && (k & known) == top);
+        higher += __popcll(__ballot(in && (k & known) > top));
+        if (same == 0) return;
+        if ((same >> lane) & 1) {
+          const int at = listed + __popcll(same & (((uint64_t)1 << lane) - 1));
+          if (at < kListed) lds.list[wave][at] = k;
+          count_digit(k);
+        }
+        listed += __popcll(same);
+      });
+      if (listed > kListed && lane == 0) lds.over = 1;  // (cleared before the passes)
+    } else if (kPer == 0 && shift == 0 && !lds.over) {
+      for (int i = lane; i < listed; i += kWave) {
+        const uint32_t k = lds.list[wave][i];
+        if ((k & known) == top) count_digit(k);
+      }
+    } else {
+      each([&](int, uint32_t k, float, bool in) {
+        if (in && (k & known) == top) count_digit(k);
+      });
+    }
     __syncthreads();
     // the bins from the highest down, kEach a thread: where the count reaches `need`
     const int hb = kBins - 1 - kEach * tid;
@@ -178,11 +212,22 @@ __device__ __forceinline__ void select_row(const Keep &n, const float *scores, S
   // Kept: keys above `top`, and of those equal to it (in its known digits) all,
   // or the first `need` by position.
   uint32_t above = 0, equal = 0;
-  each([&](int, uint32_t key, float, bool in) {
-    const uint32_t k = key & known;
-    above += __popcll(__ballot(in && k > top));
-    equal += __popcll(__ballot(in && k == top));
-  });
+  const bool by_list = kPer == 0 && (known << kDigit) != 0 && !lds.over;  // (two digits or more are known)
+  if (by_list) {
+    above = higher;
+    for (int i0 = 0; i0 < listed; i0 += kWave) {
+      const bool in = i0 + lane < listed;
+      const uint32_t k = in ? lds.list[wave][i0 + lane] & known : 0;
+      above += __popcll(__ballot(in && k > top));
+      equal += __popcll(__ballot(in && k == top));
+    }
+  } else {
+    each([&](int, uint32_t key, float, bool in) {
+      const uint32_t k = key & known;
+      above += __popcll(__ballot(in && k > top));
+      equal += __popcll(__ballot(in && k == top));
+    });
+  }
   __syncthreads();  // (wsum has been read)
   if (lane == 0) {
     wsum[0][wave] = above;
@@ -219,7 +264,7 @@ __device__ __forceinline__ KeptRow kept_row(const EvictParams &p, int64_t row) {
 
 template <int kPer>
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictParams p) {
-  __shared__ SelectLds lds;
+  __shared__ SelectLds<kPer> lds;
   const int b = (int)(blockIdx.x / p.hkv), g = (int)(blockIdx.x - (int64_t)b * p.hkv);
   const Keep n = keep_of(p, b);
   if (g == 0 && threadIdx.x == 0) p.new_lens[b] = n.keep;
@@ -396,7 +441,7 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictParams p)
 template <int kPer, int kB>
 __global__ __launch_bounds__(kSelectThreads) void evict_small_kernel(EvictParams p) {
   using M = Move<kB, 8, kSelectWaves / 2, kSelectWaves / 2, kB == 32 ? 8 : 4>;
-  __shared__ SelectLds lds;
+  __shared__ SelectLds<kPer> lds;
   __shared__ typename M::Lds s;
   __shared__ int s_kept[kSlots];
   __shared__ int s_pages[kPer * kSelectThreads / kB];  // the row of the source's table

@@ -99,6 +99,21 @@ def test_kv_evict(gpu_lib, pg, kind):
     e.check(s, budgets, 8, 4)
 
 
+@pytest.mark.parametrize("pg", [16, 32, 256])
+@pytest.mark.parametrize("longest,max_keep,kind", [(1500, 600, "ties"), (5000, 600, "spread"), (5000, 200, "odd"),
+                                                   (16384, 70, "ties"), (17000, 70, "spread"), (40000, 70, "ties")])
+def test_kv_evict_sizes(gpu_lib, longest, max_keep, kind, pg):
+    """Contexts up to and past 4K and 16K, with few slots in all and many (more
+    than 256 runs of 32)."""
+    print(f"[evict-sizes] pg={pg} longest={longest} max_keep={max_keep} {kind}", flush=True)
+    lens = [0, 33, 777, 1024, 600, 1025, 63, longest]
+    budgets = [9, 33, 32, max_keep, 500, 61, 64, max_keep]
+    e = Evict(lens, max_keep, 2, pg, (1320, pg, longest))
+    s = _scores(len(lens), 2, longest, (5, pg), kind)
+    e.run(s, budgets, 20, 3)
+    e.check(s, budgets, 20, 3)
+
+
 @pytest.mark.parametrize("recent,sinks,budgets", [(0, 0, [0, 1, 31, 32, 33, 500]), (0, 3, [2, 3, 4, -5, 90, 90]),
                                                   (40, 0, [39, 40, 41, 80, 90, 0]), (1000, 1000, [7, 50, 90, 90, 1, 2]),
                                                   (30, 20, [10, 30, 45, 50, 51, 90])])
