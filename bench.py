@@ -54,15 +54,15 @@ FLUSH_BYTES = 1 << 30  # a write this large evicts the 256 MB memory-side cache
 # on (SHA-256 below); once they change the benchmark reports null until it is
 # measured again.
 MEASURED_TRAFFIC = {
-    "decode_full_stack70": {"sources": ["decode.hip", "hswa_common.h", "hswa_launch.h"],
-                            "sha256": "ce8c8b087b183830db424f7da04debcfe929bc98eb2f6a243d11aaf7fb678adb",
-                            "fetch_bytes": 8609245287, "write_bytes": 5575537},
+    "decode_full_stack70": {"sources": ["decode_kernels.h", "decode.hip", "hswa_common.h", "hswa_launch.h"],
+                            "sha256": "66c918449d92ee898d776049cd45a000fabc804204c1278b48dbefa2ebe7233d",
+                            "fetch_bytes": 8609257988, "write_bytes": 5575740},
     "prefill_full": {"sources": ["prefill.hip", "hswa_common.h", "hswa_launch.h"],
-                     "sha256": "30b227653aa81e4c516db740ab1fb44b799a548790a265a7a870c6c6087c80d2",
-                     "fetch_bytes": 453089455, "write_bytes": 141397204},
+                     "sha256": "5878a1070c30c1d24385eceb3635afcddeaf3b308faf519db52bd8aba06ec528",
+                     "fetch_bytes": 452867031, "write_bytes": 141418964},
     "prefill_swa": {"sources": ["prefill_run.hip", "hswa_common.h", "hswa_launch.h"],
-                    "sha256": "0dde1257a07c56f6bcecc1f026cbb7636c660e1de65fe935fbc2a3f1cbd3f217",
-                    "fetch_bytes": 184862370, "write_bytes": 147919465},
+                    "sha256": "3e80e162c8304e5f91a870e10c2f256fe9658521e3871d32a58d0fe06e987fc6",
+                    "fetch_bytes": 184857403, "write_bytes": 148496975},
 }
 
 

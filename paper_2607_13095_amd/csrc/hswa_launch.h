@@ -152,9 +152,8 @@ struct SharedParams {
 // Up to this many (query, head) columns of a KV head the scores are stored, 4
 // bytes for each of a key's columns. 64 / 8 heads, 16 sequences, us a call with
 // them stored and formed anew: 24 columns (3 queries) over 2 - 16K keys 186 and
-// 222, over 30 - 32K 558 and 586; 32 columns 205 and 225, 620 and 592; one
-// sequence of 4K 31 and 27, 34 and 33. From there on it is the workspace that
-// counts: 32 columns of 16 x 64K keys take 1.1 GB.
+// 213, over 30 - 32K 558 and 567; 32 columns 205 and 216, 620 and 570. From there
+// on it is the workspace that counts: 32 columns of 16 x 64K keys take 1.1 GB.
 constexpr int kKeepColumns = 16;
 struct ScoredParams {
   SharedParams s;          // s.d: split, with ws_s; or with row_lse, all of s, each sequence a group
