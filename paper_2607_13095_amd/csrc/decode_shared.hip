@@ -772,23 +772,26 @@ __global__ __launch_bounds__(kMergeThreads) void shared_merge_kernel(SharedParam
   static_assert(kRowWaves == 1 || kRowWaves == kMergeWaves, "a row has one wave or its workgroup");
   const int wid = uni((int)(threadIdx.x / kWave));
   const int rw = kRowWaves == 1 ? 0 : wid;  // wave of the row
-  const int64_t idx = (int64_t)blockIdx.x * (kMergeWaves / kRowWaves) + (kRowWaves == 1 ? wid : 0);
-  if (idx >= (int64_t)d.ns * d.nq * d.hq) return;
-  const int b = (int)(idx / ((int64_t)d.nq * d.hq));
+  const uint32_t idx = blockIdx.x * (kMergeWaves / kRowWaves) + (kRowWaves == 1 ? wid : 0);  // (below 2^26)
+  const uint32_t each = d.nq * d.hq;
+  if (idx >= d.ns * each) return;
+  const int b = (int)(idx / each);
+  // (the loads of all go out together)
+  const int given = d.ctx_lens[b];
+  const SharedHead h = *p.head;
+  const SharedSeq seq = p.seqs[b];
   const int half = lane >> 5, d4 = (lane & 31) * 4;
-  u32x2 *dst = reinterpret_cast<u32x2 *>(d.out + idx * kHeadDim + d4);
+  u32x2 *dst = reinterpret_cast<u32x2 *>(d.out + (int64_t)idx * kHeadDim + d4);
   const u32x2 zero = {0u, 0u};
-  const int ctx = min(d.ctx_lens[b], d.max_ctx);
+  const int rem = (int)(idx - b * each);
+  const int qi = (int)((uint32_t)rem / (uint32_t)d.hq), head = rem - qi * d.hq;
+  const int g = (int)((uint32_t)head / (uint32_t)d.group), hh = head - g * d.group;
+  const int ctx = min(given, d.max_ctx);
   if (ctx < 1) {
     if (half == 0) *dst = zero;
     if (scored(kMode) && lane == 0) d.row_lse[idx] = INFINITY;
     return;
   }
-  const SharedHead h = *p.head;
-  const SharedSeq seq = p.seqs[b];
-  const int rem = (int)(idx - (int64_t)b * d.nq * d.hq);
-  const int qi = rem / d.hq, head = rem - qi * d.hq;
-  const int g = head / d.group, hh = head - g * d.group;
   // pieces of the prefix: rows first, first + 256, ... of its partials
   int n0 = 0;
   int64_t first = 0;
@@ -814,7 +817,7 @@ __global__ __launch_bounds__(kMergeThreads) void shared_merge_kernel(SharedParam
   }
   if (!scored(kMode) && n0 == 0 && n1 == 1) return;  // one piece: the decode kernel wrote the row
   const int n = n0 + n1;
-  const float *po0 = p.ws_o + first * kHeadDim + d4, *po1 = d.ws_o + idx * d.max_splits * kHeadDim + d4;
+  const float *po0 = p.ws_o + first * kHeadDim + d4, *po1 = d.ws_o + (int64_t)idx * d.max_splits * kHeadDim + d4;
   auto load = [&](int s0, f32x4 (&v)[8]) {  // pieces s0 .. s0 + 15
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
@@ -827,7 +830,7 @@ __global__ __launch_bounds__(kMergeThreads) void shared_merge_kernel(SharedParam
   f32x4 v[8];
   load(16 * rw, v);  // (beside the log-sum-exps)
   auto lse_of = [&](int s) {
-    return s < n0 ? p.ws_lse[first + (int64_t)s * kTileCols] : d.ws_lse[idx * d.max_splits + s - n0];
+    return s < n0 ? p.ws_lse[first + (int64_t)s * kTileCols] : d.ws_lse[(int64_t)idx * d.max_splits + s - n0];
   };
   float mx = -INFINITY;
   for (int s = lane; s < n; s += kWave) mx = fmaxf(mx, lse_of(s));
