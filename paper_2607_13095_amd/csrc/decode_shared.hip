@@ -265,8 +265,107 @@ __device__ __forceinline__ void plan_small(const SharedParams &p, SmallPlan &at)
   }
 }
 
+// The plan of a batch of up to kPlanThreads sequences and fewer groups, a thread
+// each. (us a call with it and with the loops below: 90 sequences in 3 groups 60.8
+// and 63.2, 256 in 100 groups 132.2 and 138.8, 64 / 8 heads; 200 in 30, 8 / 1, 43.1
+// and 46.6.)
+struct BlockPlan {
+  int64_t part[kPlanWaves];
+  int32_t cut[kPlanThreads];
+  int32_t least[kPlanThreads], count[kPlanThreads], leader[kPlanThreads];
+  SharedGroup groups[kPlanThreads];
+  int64_t units[kPlanThreads], rows[kPlanThreads];
+};
+__device__ __forceinline__ void plan_block(const SharedParams &p, BlockPlan &at) {
+  const DecodeParams &d = p.d;
+  const int tid = threadIdx.x;
+  const auto add = [](int64_t a, int64_t b) { return a + b; };
+  const auto most = [](int64_t a, int64_t b) { return max64(a, b); };
+  const int ctx = tid < d.ns ? min(d.ctx_lens[tid], d.max_ctx) : 0;
+  const int shared = tid < p.ng ? group_shared(p, tid) : 0;
+  // offsets that are out of range or decrease make empty groups, never overlapping ones
+  const int cut = tid <= p.ng ? min(max(group_first(p, tid), 0), d.ns) : 0;
+  int64_t last;
+  at.cut[tid] = (int)block_scan(cut, at.part, last, most);
+  at.least[tid] = at.leader[tid] = INT32_MAX;
+  at.count[tid] = 0;
+  __syncthreads();
+  int grp = 0;  // of sequence `tid`: the last group that starts at or before it
+  for (int hi = p.ng; hi - grp > 1;) {
+    const int mid = (grp + hi) >> 1;
+    if (at.cut[mid] <= tid) grp = mid;
+    else hi = mid;
+  }
+  const bool member = tid >= at.cut[0] && tid < at.cut[p.ng] && ctx >= 1;
+  if (member) {
+    atomicMin(&at.least[grp], ctx);
+    atomicMin(&at.leader[grp], tid);
+    atomicAdd(&at.count[grp], 1);
+  }
+  __syncthreads();
+  SharedGroup g{};
+  if (tid < p.ng) {
+    const int n = at.cut[tid + 1] - at.cut[tid];
+    g.first = at.cut[tid];
+    g.leader = at.count[tid] > 0 ? at.leader[tid] : 0;
+    g.tiles = g.padded = n > 0 ? shared_tiles(p, shared, at.least[tid], at.count[tid]) : 0;
+    g.cols = g.tiles > 0 ? n * d.nq * d.group : 0;
+    at.groups[tid] = g;
+  }
+  __syncthreads();
+  const int start = member ? at.groups[grp].tiles * kKT : 0;
+  const int nch = ctx >= 1 ? (ctx - start + kChunk - 1) / kChunk : 0;
+  const int H = d.hkv * ((d.nq * d.group + d.item_cols - 1) / d.item_cols);
+  int64_t chunks, longest;
+  const int64_t before = (block_scan(nch, at.part, chunks, add) - nch) * H;
+  block_scan(nch, at.part, longest, most);
+  int64_t units = 0, rows = 0, all_units = 0, cost = 0;
+  if (p.ng >= kWave) {
+    const int64_t gu = (int64_t)d.hkv * ((g.cols + kTileCols - 1) / kTileCols) * g.tiles;
+    const int64_t gr = (int64_t)d.hkv * ((g.cols + kCols - 1) / kCols * kCols);
+    units = block_scan(gu, at.part, all_units, add) - gu;
+    rows = block_scan(gr, at.part, last, add) - gr;
+    block_scan(d.hkv * cols_cost(g.cols) * g.tiles, at.part, cost, add);
+  }
+  if (tid < kWave) {
+    const SharedHead h = p.ng < kWave ? plan_groups(p, g, chunks * H, longest, units, rows)
+                                      : divide_work(d, all_units, cost, chunks * H, longest);
+    if (tid == 0) {
+      p.group_units[p.ng] = h.units;
+      *p.head = h;
+    }
+  }
+  if (tid < p.ng) {
+    p.groups[tid] = at.groups[tid] = g;
+    p.group_units[tid] = at.units[tid] = units;
+    p.group_rows[tid] = at.rows[tid] = rows;
+  }
+  __syncthreads();
+  if (tid >= d.ns) return;
+  SharedSeq q{};
+  q.start = start;
+  q.own_units = before;
+  if (start > 0) {
+    g = at.groups[grp];
+    q.col = (tid - g.first) * d.nq * d.group;
+    q.tiles = g.tiles;
+    q.padded = g.padded;
+    q.cols = g.cols;
+    q.units = at.units[grp];
+    q.rows = at.rows[grp];
+  }
+  p.start[tid] = start;
+  p.own_units[tid] = before;
+  p.seqs[tid] = q;
+}
+
 __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(SharedParams p) {
-  __shared__ int64_t part[kPlanWaves];
+  __shared__ BlockPlan plan;
+  if (p.d.ns <= kPlanThreads && p.ng < kPlanThreads) {
+    plan_block(p, plan);
+    return;
+  }
+  auto &part = plan.part;
   __shared__ int32_t cut[kPlanThreads + 1];  // first sequences of the groups at hand, made non-decreasing
   const auto add = [](int64_t a, int64_t b) { return a + b; };
   const auto most = [](int64_t a, int64_t b) { return max64(a, b); };

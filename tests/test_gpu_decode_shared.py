@@ -177,6 +177,26 @@ def test_decode_shared_many_groups(gpu_lib):
     s.check(s.run(), "many groups")
 
 
+@pytest.mark.parametrize("n,ng", [(64, 63), (65, 1), (66, 64), (100, 63), (130, 64), (256, 255), (257, 256), (257, 20)])
+def test_decode_shared_batches(gpu_lib, n, ng):
+    """Batches and group counts about the sizes at which the plan is found
+    another way; members without a context; offsets that decrease."""
+    print(f"[shared-batches] n={n} ng={ng}", flush=True)
+    r = np.random.default_rng(n + ng)
+    cuts = [0] + sorted(int(x) for x in r.choice(np.arange(1, n), ng - 1, replace=False)) + [n]
+    groups = [(int(r.integers(60, 400)), [int(x) for x in r.integers(1, 90, b - a)]) for a, b in zip(cuts, cuts[1:])]
+    s = Shared(groups, 1, 8, 1, 64, (1520, n, ng))
+    s.check(s.run(), f"{n} sequences in {ng} groups")
+    ctx = [0 if r.random() < 0.2 else c for c in s.ctx]
+    s.check(s.run(ctx=ctx), f"{n} sequences in {ng} groups, some without a context")
+    if ng >= 20:
+        cu = [int(x) for x in s.cu]
+        cu[10], cu[11] = cu[11], cu[9]  # (group 9 would reach into group 10's: it shares what both have)
+        shared = list(s.shared)
+        shared[9] = 0
+        s.check(s.run(cu=cu, shared=shared, ctx=ctx), f"{n} sequences in {ng} groups, decreasing")
+
+
 def test_decode_shared_copied_prefix(gpu_lib):
     """Rows that hold copies of the prefix in pages of their own."""
     lens = [900, 1000, 905]
