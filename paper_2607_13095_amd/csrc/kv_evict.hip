@@ -64,11 +64,11 @@ __device__ __forceinline__ uint32_t score_key(float s) {
 // selection and 47; 2 x 130K to 2000: 164 us a call and 141).
 template <int kPer>
 struct SelectLds {
-  uint32_t hist[kBins * kCopies];
+  alignas(16) uint32_t hist[kBins * kCopies];  // (16-byte reads)
   uint32_t wsum[2][kSelectWaves];
   uint32_t found[3];
-  uint32_t over;                                              // (kPer 0) whether a wave's list is too short
-  uint32_t list[kSelectWaves][kPer == 0 ? kListed : 1];       // keys of the first digit sought, in order
+  uint32_t over;                                         // (kPer 0) whether a wave's list is too short
+  uint32_t list[kSelectWaves][kPer == 0 ? kListed : 1];  // keys of the first digit sought, in order
 };
 // emit(slot, position, score) for every kept key of row (b, g), by kSelectThreads.
 template <int kPer, typename Emit>
