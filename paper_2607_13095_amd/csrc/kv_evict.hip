@@ -61,7 +61,7 @@ __device__ __forceinline__ uint32_t score_key(float s) {
 // that share the first digit sought (a twentieth of them, if the scores spread over
 // some orders of magnitude), for the third digit and the counts: three passes
 // instead of five, unless a wave's list is too short (8 x 58K, 8 KV heads: 54 us of
-// selection and 47; 2 x 130K to 2000: 164 us a call and 141).
+// selection and 48; 2 x 130K to 2000: 164 us a call and 138).
 template <int kPer>
 struct SelectLds {
   alignas(16) uint32_t hist[kBins * kCopies];  // (16-byte reads)
@@ -434,10 +434,10 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictParams p)
 // Both for few slots: every workgroup selects for its row by itself and moves
 // its 32 slots, half of the waves K and half V; the second launch and the way of
 // the positions through memory are saved. us a call, one kernel and two (8 KV
-// heads): 1 x 1000 to 300 11.1 and 14.2, 1 x 4100 to 1024 15.1 and 17.5, 1 x 16000
-// to 1000 27.2 and 30.8, 32 x 300 to 30 15.9 and 19.9; with more workgroups than
-// compute units (two in LDS do not fit one) 2 x 4000 to 1000 26.4 and 21.2.
-// kPer as above, 1 or more.
+// heads): 1 x 1000 to 300 9.7 and 12.7, 1 x 4100 to 1024 13.6 and 16.0, 1 x 16000
+// to 1000 25.2 and 29.0, 32 x 300 to 30 14.5 and 18.5; with more workgroups than
+// compute units (two in LDS do not fit one) 2 x 4000 to 1000 23.1 and 19.5.
+// kPer as above, not 0.
 template <int kPer, int kB>
 __global__ __launch_bounds__(kSelectThreads) void evict_small_kernel(EvictParams p) {
   using M = Move<kB, 8, kSelectWaves / 2, kSelectWaves / 2, kB == 32 ? 8 : 4>;
@@ -472,30 +472,40 @@ __global__ __launch_bounds__(kSelectThreads) void evict_small_kernel(EvictParams
   M::run(p, s, g, s0, count);
 }
 
+template <int kPer>
+hipError_t launch_small(const EvictParams &p, int64_t items, hipStream_t stream) {
+  const dim3 grid((unsigned)items), threads(kSelectThreads);
+  return p.src.vb_shift == 4 ? launch_kernel(evict_small_kernel<kPer, 16>, grid, threads, stream, p)
+                             : launch_kernel(evict_small_kernel<kPer, 32>, grid, threads, stream, p);
+}
+
+template <int kPer>
+hipError_t launch_select(const EvictParams &p, hipStream_t stream) {
+  return launch_kernel(evict_select_kernel<kPer>, dim3((unsigned)(p.ns * p.hkv)), dim3(kSelectThreads), stream, p);
+}
+
 }  // namespace
 
 hipError_t launch_kv_evict(const EvictParams &p, hipStream_t stream) {
-  const dim3 rows((unsigned)(p.ns * p.hkv)), threads(kSelectThreads);
   const int64_t items = (int64_t)((p.max_keep + kSlots - 1) / kSlots) * p.ns * p.hkv;
-  // scores in registers as far as they fit
-  if (items <= kSmallItems && p.max_ctx <= 16 * kSelectThreads) {
-    const dim3 grid((unsigned)items);
-    const bool few = p.max_ctx <= 4 * kSelectThreads;
-    if (p.src.vb_shift == 4)
-      return few ? launch_kernel(evict_small_kernel<4, 16>, grid, threads, stream, p)
-                 : launch_kernel(evict_small_kernel<16, 16>, grid, threads, stream, p);
-    return few ? launch_kernel(evict_small_kernel<4, 32>, grid, threads, stream, p)
-               : launch_kernel(evict_small_kernel<16, 32>, grid, threads, stream, p);
-  }
-  hipError_t e;
-  if (p.max_ctx <= 4 * kSelectThreads) e = launch_kernel(evict_select_kernel<4>, rows, threads, stream, p);
-  else if (p.max_ctx <= 16 * kSelectThreads) e = launch_kernel(evict_select_kernel<16>, rows, threads, stream, p);
-  else e = launch_kernel(evict_select_kernel<0>, rows, threads, stream, p);
+  // Scores in registers as far as they fit: us a call with 8, 16, 32 of them and by
+  // passes, 1 x 6000 to 1000, 1 KV head, 13.7 and 14.8; 1 x 16000 to 1000, 8 KV heads,
+  // 25.2 (16) and 28.1 (32); 1 x 20000 30.6 (32) and 35.8 (passes).
+  const int per = (p.max_ctx + kSelectThreads - 1) / kSelectThreads;
+  if (items <= kSmallItems && per <= 32)
+    return per <= 8    ? launch_small<8>(p, items, stream)
+           : per <= 16 ? launch_small<16>(p, items, stream)
+                       : launch_small<32>(p, items, stream);
+  const hipError_t e = per <= 8    ? launch_select<8>(p, stream)
+                       : per <= 16 ? launch_select<16>(p, stream)
+                       : per <= 32 ? launch_select<32>(p, stream)
+                                   : launch_select<0>(p, stream);
   if (e != hipSuccess) return e;
   const dim3 grid((unsigned)std::min<int64_t>(items, kMaxMoveGrid)), block(kMoveThreads);
   // With a workgroup per compute unit or fewer, more blocks at a time save waits
-  // (1 x 4K to 1024, 8 KV heads: 9.7 and 8.5 us); with more of them, four leave
-  // room in LDS for three on a unit (16 x 16K: 194 us, with eight 340).
+  // (us a call with eight and four: 1 x 40000 to 4000, 1 KV head, 41.8 and 43.7; 1 x
+  // 20000 to 1000, 8 of them, 36.1 and 38.0); with more of them, four leave room in
+  // LDS for three on a unit (16 x 16K: the move 340 and 194).
   const bool few = items <= 256;
   if (p.src.vb_shift == 4)
     return few ? launch_kernel(evict_move_kernel<16, 8>, grid, block, stream, p)

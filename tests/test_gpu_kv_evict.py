@@ -101,9 +101,10 @@ def test_kv_evict(gpu_lib, pg, kind):
 
 @pytest.mark.parametrize("pg", [16, 32, 256])
 @pytest.mark.parametrize("longest,max_keep,kind", [(1500, 600, "ties"), (5000, 600, "spread"), (5000, 200, "odd"),
-                                                   (16384, 70, "ties"), (17000, 70, "spread"), (40000, 70, "ties")])
+                                                   (16384, 70, "ties"), (17000, 70, "spread"), (40000, 70, "ties"),
+                                                   (9000, 600, "spread"), (20000, 600, "odd"), (32768, 70, "equal")])
 def test_kv_evict_sizes(gpu_lib, longest, max_keep, kind, pg):
-    """Contexts up to and past 4K and 16K, with few slots in all and many (more
+    """Contexts up to and past 8K, 16K and 32K, with few slots in all and many (more
     than 256 runs of 32)."""
     print(f"[evict-sizes] pg={pg} longest={longest} max_keep={max_keep} {kind}", flush=True)
     lens = [0, 33, 777, 1024, 600, 1025, 63, longest]
