@@ -146,7 +146,7 @@ struct SharedGeometry {
 
 SharedGeometry shared_geometry(const hswa_shape *sh, int32_t ns, int32_t max_ctx, int32_t nq, int32_t ng) {
   SharedGeometry g{};
-  g.d = decode_geometry(sh, ns, max_ctx, nq, true);
+  g.d = decode_geometry(sh, ns, max_ctx, nq, true, 128);
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t o = at;
