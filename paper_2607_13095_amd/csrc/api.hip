@@ -207,15 +207,16 @@ ScoredGeometry scored_geometry(const hswa_shape *sh, int32_t ns, int32_t max_ctx
 // some 12 us more than a short decode, which reading less has to make up for, at
 // most (ns - num_groups) * max_shared_len positions of every KV head. us by prefix
 // and by hswa_decode_multi, 100 - 300 own tokens, with the MB saved (shared keys):
-//   64 / 8 heads   2 sequences x 8000      33 MB   26 / 22
-//                  2 x 16000               66      29 / 32
-//                  4 x 4000, 4 x 8000      49, 98  24 / 21, 27 / 30
-//                  8 x 2000, 8 x 4000      57, 115 26 / 22, 27 / 29
-//                  8 in 4 groups x 4000    66      37 / 32
-//                  32 x 1000               127     30 / 32
-//   8 / 1          8 x 16000, 8 x 32000    57, 115 23 / 20, 26 / 29
-//   16 / 16        2 x 4000, 2 x 8000      33, 66  24 / 22, 27 / 31
-//                  32 x 256                65      27 / 27
+//   64 / 8 heads   2 sequences x 8000      33 MB   23 / 22
+//                  2 x 16000               66      25 / 34
+//                  4 x 4000, 4 x 8000      49, 98  22 / 22, 24 / 31
+//                  8 x 2000, 8 x 4000      57, 115 23 / 22, 23 / 31
+//                  8 in 4 groups x 4000    66      28 / 33
+//                  32 x 1000               127     27 / 33
+//   8 / 1          8 x 16000, 8 x 32000    57, 115 21 / 21, 23 / 31
+//                  32 x 4000               63      24 / 20
+//   16 / 16        2 x 4000, 2 x 8000      33, 66  21 / 22, 24 / 31
+//                  32 x 256                65      25 / 28
 bool shared_fits(const hswa_shape *sh, int32_t ns, int32_t num_groups, int32_t max_context_len,
                  int32_t max_shared_len) {
   constexpr double kLeastSaved = 70e6;

@@ -54,14 +54,17 @@ constexpr int kMinSpan = 4;         // least key tiles of a span
 constexpr int kMinOwn = 4;          // least chunks of a span of the own keys
 constexpr int kXcds = 8;
 constexpr int kWorkWaves = kThreads / kWave;
-// What work takes, in 0.1 us (measured in place): a key tile under up to 128 and
-// under 256 columns; a workgroup's start and end on a span of them; a wave's chunk
-// of own keys with the other seven at work too (50 GB/s, what a compute unit gets
-// from HBM, whatever is in flight) and its start; all compute units' share of a
-// chunk at 5.5 TB/s; the merge of a prefix workgroup's partials.
-constexpr int kCostHalf = 10, kCostFull = 19;
+// What work takes, in 0.1 us (measured in place, with the other kind at work too; the
+// slowest workgroups count): a key tile under up to 128 and under 256 columns; a
+// workgroup's start and end on a span of them; a wave's chunk of own keys with the
+// other seven at work (50 GB/s, what a compute unit gets from HBM whatever is in
+// flight, would be 26) and its start; all compute units' share of a chunk at 5.5
+// TB/s; the merge of a prefix workgroup's partials. (Against means, 10, 26 and 65
+// for the first, the chunk and its start: 32 x (8192 + 100 - 1500) 40.9 us, now 38.4;
+// 64 x (64K + 200 - 2000) 184, 178; 90 in 3 groups 60.8, 57.0.)
+constexpr int kCostHalf = 14, kCostFull = 19;
 constexpr float kCostSpan = 115.f;
-constexpr float kCostOwn = 26.f, kCostOwnStart = 65.f, kCostOwnHbm = .03f, kCostMerge = .4f;
+constexpr float kCostOwn = 33.f, kCostOwnStart = 85.f, kCostOwnHbm = .03f, kCostMerge = .4f;
 constexpr int kAlignedGroups = 16;  // up to this many groups the plan looks for spans that end with the tiles
 
 __device__ __forceinline__ int64_t max64(int64_t a, int64_t b) { return a > b ? a : b; }
