@@ -17,7 +17,7 @@
 //           The plan (plan_small) divides the compute units between the two by
 //           what each has to do, so that matrix products and reads run side by
 //           side. (As kernels one after the other, 32 sequences of 100 - 1500
-//           own keys over 8192 shared ones took 23 + 26 us, 41 so.)
+//           own keys over 8192 shared ones took 23 + 26 us and their merge, all 38 so.)
 //   merge   the partials of each row
 // Every workgroup finds the plan by itself, in one wave: a kernel for it
 // took 9 us. Batches of more than 64 sequences or 63 groups (or 2^31 own chunks)
