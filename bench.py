@@ -55,14 +55,14 @@ FLUSH_BYTES = 1 << 30  # a write this large evicts the 256 MB memory-side cache
 # measured again.
 MEASURED_TRAFFIC = {
     "decode_full_stack70": {"sources": ["decode_kernels.h", "decode.hip", "hswa_common.h", "hswa_launch.h"],
-                            "sha256": "66c918449d92ee898d776049cd45a000fabc804204c1278b48dbefa2ebe7233d",
-                            "fetch_bytes": 8609257988, "write_bytes": 5575740},
+                            "sha256": "db90c0e4d02000fca79586e644b544144f0c6ce35d5c618a508afdb7993d1f0f",
+                            "fetch_bytes": 8609234479, "write_bytes": 5574350},
     "prefill_full": {"sources": ["prefill.hip", "hswa_common.h", "hswa_launch.h"],
-                     "sha256": "5878a1070c30c1d24385eceb3635afcddeaf3b308faf519db52bd8aba06ec528",
-                     "fetch_bytes": 452867031, "write_bytes": 141418964},
+                     "sha256": "361c9927c2011310a59e80866afa7d153ff85834f6570c094696ea09f44561fc",
+                     "fetch_bytes": 452863023, "write_bytes": 141388810},
     "prefill_swa": {"sources": ["prefill_run.hip", "hswa_common.h", "hswa_launch.h"],
-                    "sha256": "3e80e162c8304e5f91a870e10c2f256fe9658521e3871d32a58d0fe06e987fc6",
-                    "fetch_bytes": 184857403, "write_bytes": 148496975},
+                    "sha256": "0fc0198dc3887a979c26c093b9e4c18919f475136d76e63f15ec6049d97bdbe6",
+                    "fetch_bytes": 184857995, "write_bytes": 147068669},
 }
 
 

@@ -420,7 +420,7 @@ __device__ __forceinline__ void decode_waves(const DecodeParams &p, [[maybe_unus
       int64_t kept_to = 0;  // where the next run goes, in 16-byte pieces
       if constexpr (kMode == kKept) kept_to = uni64((((int64_t)b * hkv + g) * p.max_chunks + c_lo) * ncols * 8);
       auto store_kept = [&]() {
-        __builtin_amdgcn_wave_barrier();
+        wave_exchange();
         const int n = kept * ncols * 8;
         const __amdgpu_buffer_rsrc_t rs =
             __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<f32x4 *>(p.ws_s) + kept_to, 0, n * 16, kBufferWord3);
@@ -428,7 +428,7 @@ __device__ __forceinline__ void decode_waves(const DecodeParams &p, [[maybe_unus
           __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, s_keep[wid][i]), rs, i * 16, 0, kWriteThrough);
         kept_to += n;
         kept = 0;
-        __builtin_amdgcn_wave_barrier();
+        wave_exchange();
       };
 
       // QK^T and the online softmax of one chunk: returns P^T packed as bf16 and

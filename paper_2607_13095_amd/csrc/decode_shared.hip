@@ -201,9 +201,9 @@ __device__ __forceinline__ void plan_small(const SharedParams &p, SmallPlan &at)
   grp = member ? grp : -1;
   // the shortest context of each group
   at.least[lane] = INT32_MAX;
-  __builtin_amdgcn_wave_barrier();
+  wave_exchange();
   if (member && ctx >= 1) atomicMin(&at.least[grp], ctx);
-  __builtin_amdgcn_wave_barrier();
+  wave_exchange();
   const uint64_t live = __ballot(ctx >= 1);
   const uint64_t upto = end >= 64 ? ~0ull : ((uint64_t)1 << end) - 1;
   const bool group = lane < p.ng && cut < end;

@@ -172,6 +172,16 @@ __device__ __forceinline__ float last_lane(float x) {
   return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), kWave - 1));
 }
 
+// Exchange of LDS data among the lanes of one wave: what each of them stored (or
+// took part in by an atomic) before is what all of them load after. The barrier
+// alone orders no memory: a lane's load after it might be given that lane's own
+// store before it. The hardware takes a wave's LDS accesses in order, so the
+// fences cost no wait.
+__device__ __forceinline__ void wave_exchange() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 
 constexpr float kLog2e = 1.4426950408889634f;
 

@@ -366,7 +366,7 @@ struct Move {
         for (int l = 0; l < kLoads; ++l)
           ld[k][l] = b0 + k < blocks && page >= 0 ? ldg128(src + (l * kWave + lane) * 8) : z;
       }
-      __builtin_amdgcn_wave_barrier();  // (the picks from the blocks before are done)
+      wave_exchange();  // (the picks from the blocks before are done)
 #pragma unroll
       for (int k = 0; k < kStageBlocks; ++k)
 #pragma unroll
@@ -374,7 +374,7 @@ struct Move {
           const int x = l * kWave + lane;
           s.stage[vw][k][x / kRow * kPad + x % kRow] = ld[k][l];
         }
-      __builtin_amdgcn_wave_barrier();
+      wave_exchange();
 #pragma unroll
       for (int e = 0; e < kPick; ++e) {
         const int blk = s.block[i0 + e] - b0;
@@ -383,7 +383,7 @@ struct Move {
         const uint32_t v = rowp[s.off[i0 + e] & (kB - 1)];
         if (blk >= 0 && blk < kStageBlocks) val[e >> 1] |= v << (16 * (e & 1));
       }
-      __builtin_amdgcn_wave_barrier();
+      wave_exchange();
     }
     const int to = s.to[i0];
     if (to < 0) return;
