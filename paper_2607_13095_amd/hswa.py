@@ -534,6 +534,14 @@ def _queries(q, context_lens):
     return int(q.shape[0]), int(q.shape[1]) if q.dim() == 4 else 1
 
 
+def _int32(x, name: str) -> int:
+    """A host integer as the C ABI takes it (ctypes would keep its low 32 bits)."""
+    x = int(x)
+    if not -(1 << 31) <= x < 1 << 31:
+        raise ValueError(f"{name} = {x} does not fit 32 bits")
+    return x
+
+
 def _workspace(workspace):
     if workspace is None:
         return None, 0
@@ -542,8 +550,9 @@ def _workspace(workspace):
 
 def decode_shared_workspace_bytes(shape: Shape, ns: int, num_queries: int, max_context_len: int, num_groups: int,
                                   max_shared_len: int) -> int:
-    return int(load().hswa_decode_shared_workspace_bytes(shape.ref(), int(ns), int(num_queries), int(max_context_len),
-                                                         int(num_groups), int(max_shared_len)))
+    return int(load().hswa_decode_shared_workspace_bytes(
+        shape.ref(), _int32(ns, "ns"), _int32(num_queries, "num_queries"), _int32(max_context_len, "max_context_len"),
+        _int32(num_groups, "num_groups"), _int32(max_shared_len, "max_shared_len")))
 
 
 def decode_shared(layer: Layer, shape: Shape, cache: Cache, q, context_lens, max_context_len: int, cu_groups,
@@ -554,6 +563,7 @@ def decode_shared(layer: Layer, shape: Shape, cache: Cache, q, context_lens, max
     _torch()
     ns, nq = _queries(q, context_lens)
     ng = shared_lens.numel()
+    max_ctx, max_shared = _int32(max_context_len, "max_context_len"), _int32(max_shared_len, "max_shared_len")
     if cu_groups.numel() != ng + 1:
         raise ValueError("cu_groups has one entry more than shared_lens")
     row = nq * shape.num_q_heads * shape.head_dim
@@ -563,13 +573,14 @@ def decode_shared(layer: Layer, shape: Shape, cache: Cache, q, context_lens, max
     wp, wbytes = _workspace(workspace)
     _check_cache(shape, cache, ns)
     _check_device(cache, q, context_lens, cu_groups, shared_lens, out, workspace)
-    st = load().hswa_decode_shared(layer.c(), shape.ref(), cache.ref(), qp, cp, ns, nq, int(max_context_len), gp, lp,
-                                   ng, int(max_shared_len), wp, wbytes, o, _stream(stream))
+    st = load().hswa_decode_shared(layer.c(), shape.ref(), cache.ref(), qp, cp, ns, nq, max_ctx, gp, lp, ng, max_shared,
+                                   wp, wbytes, o, _stream(stream))
     _check(st, "hswa_decode_shared")
 
 
 def decode_scored_workspace_bytes(shape: Shape, ns: int, num_queries: int, max_context_len: int) -> int:
-    return int(load().hswa_decode_scored_workspace_bytes(shape.ref(), int(ns), int(num_queries), int(max_context_len)))
+    return int(load().hswa_decode_scored_workspace_bytes(
+        shape.ref(), _int32(ns, "ns"), _int32(num_queries, "num_queries"), _int32(max_context_len, "max_context_len")))
 
 
 def decode_scored(layer: Layer, shape: Shape, cache: Cache, q, context_lens, max_context_len: int, scores_in,
@@ -585,6 +596,7 @@ def decode_scored(layer: Layer, shape: Shape, cache: Cache, q, context_lens, max
             raise TypeError("scores_out must be a torch tensor")
         if t is not None and (t.dim() != 3 or tuple(t.shape) != (ns, shape.num_kv_heads, int(scores_out.shape[-1]))):
             raise ValueError(f"{name} must be [NS, Hkv, positions] = [{ns}, {shape.num_kv_heads}, ...], both alike")
+    max_ctx, stride = _int32(max_context_len, "max_context_len"), _int32(scores_out.shape[2], "positions of scores_out")
     row = nq * shape.num_q_heads * shape.head_dim
     qp, cp = _ptr(q, "q", _BF16, ns * row), _ptr(context_lens, "context_lens", _I32, ns)
     o = _ptr(out, "out", _BF16, ns * row)
@@ -592,8 +604,8 @@ def decode_scored(layer: Layer, shape: Shape, cache: Cache, q, context_lens, max
     wp, wbytes = _workspace(workspace)
     _check_cache(shape, cache, ns)
     _check_device(cache, q, context_lens, scores_in, scores_out, out, workspace)
-    st = load().hswa_decode_scored(layer.c(), shape.ref(), cache.ref(), qp, cp, ns, nq, int(max_context_len), si, so,
-                                   int(scores_out.shape[2]), wp, wbytes, o, _stream(stream))
+    st = load().hswa_decode_scored(layer.c(), shape.ref(), cache.ref(), qp, cp, ns, nq, max_ctx, si, so, stride, wp,
+                                   wbytes, o, _stream(stream))
     _check(st, "hswa_decode_scored")
 
 
@@ -611,6 +623,10 @@ def kv_evict(layer: Layer, shape: Shape, src: Cache, dst: Cache, scores, context
             raise TypeError(f"{name} must be a torch tensor")
         if t is not None and (t.dim() != 3 or tuple(t.shape[:2]) != (ns, hkv)):
             raise ValueError(f"{name} must be [NS, Hkv, positions] = [{ns}, {hkv}, ...]")
+    max_ctx, stride = _int32(max_context_len, "max_context_len"), _int32(scores.shape[2], "positions of scores")
+    recent, sinks = _int32(num_recent, "num_recent"), _int32(num_sinks, "num_sinks")
+    most = _int32(kept_out.shape[2], "positions of kept_out")
+    out_stride = _int32(scores_out.shape[2], "positions of scores_out") if scores_out is not None else 0
     sp, kp = _ptr(scores, "scores", _F32), _ptr(kept_out, "kept_out", _I32)
     so = _ptr(scores_out, "scores_out", _F32)
     cp, bp = _ptr(context_lens, "context_lens", _I32, ns), _ptr(budgets, "budgets", _I32, ns)
@@ -619,9 +635,8 @@ def kv_evict(layer: Layer, shape: Shape, src: Cache, dst: Cache, scores, context
     _check_cache(shape, dst, ns)
     _check_device(src, dst.k_pool, dst.v_pool, dst.block_table, scores, kept_out, scores_out, context_lens, budgets,
                   new_lens_out)
-    st = load().hswa_kv_evict(layer.c(), shape.ref(), src.ref(), dst.ref(), sp, int(scores.shape[2]), cp, bp, ns,
-                              int(max_context_len), int(num_recent), int(num_sinks), kp, int(kept_out.shape[2]), so,
-                              int(scores_out.shape[2]) if scores_out is not None else 0, np_, _stream(stream))
+    st = load().hswa_kv_evict(layer.c(), shape.ref(), src.ref(), dst.ref(), sp, stride, cp, bp, ns, max_ctx, recent, sinks,
+                              kp, most, so, out_stride, np_, _stream(stream))
     _check(st, "hswa_kv_evict")
 
 
