@@ -353,7 +353,7 @@ hswa_status hswa_decode_multi(hswa_layer layer, const hswa_shape *shape, const h
  * its window), no group, one sequence, prefixes below 64, and calls whose
  * (ns - num_groups) * max_shared_len positions hold less than 70 MB, or whose
  * max_context_len is over 2^30. HSWA_ERR_UNSUPPORTED beside hswa_decode_multi's:
- * over 2^25 rows (ns * num_queries * Hq) in any other call.
+ * over 2^25 rows (ns * num_queries * Hq) in any other call (a size of 0).
  * The other arguments are as in hswa_decode_multi. */
 size_t hswa_decode_shared_workspace_bytes(const hswa_shape *shape, int32_t ns, int32_t num_queries,
                                           int32_t max_context_len, int32_t num_groups, int32_t max_shared_len);
@@ -381,7 +381,7 @@ hswa_status hswa_decode_shared(hswa_layer layer, const hswa_shape *shape, const 
  * differ from its in the last bit: their sums are not of rounded probabilities);
  * workspace >= hswa_decode_scored_workspace_bytes, for contexts of any length.
  * HSWA_ERR_UNSUPPORTED: an SWA layer (it evicts by its window), more than 2^25
- * rows (ns * num_queries * Hq), a max_context_len over 2^30. */
+ * rows (ns * num_queries * Hq), a max_context_len over 2^30 (a size of 0). */
 size_t hswa_decode_scored_workspace_bytes(const hswa_shape *shape, int32_t ns, int32_t num_queries,
                                           int32_t max_context_len);
 hswa_status hswa_decode_scored(hswa_layer layer, const hswa_shape *shape, const hswa_cache *cache, const void *q,

@@ -41,6 +41,11 @@ constexpr int64_t kMaxRows = 1 << 25;
 // Positions of a sequence whose sums of keys, tiles and spans stay within 32 bits
 constexpr int32_t kMaxLen = 1 << 30;
 
+// (their sizes of workspaces stay within 64 bits up to there)
+bool too_many_rows(const hswa_shape *sh, int32_t ns, int32_t num_queries) {
+  return (int64_t)ns * num_queries > kMaxRows / sh->num_q_heads;
+}
+
 // Shape checks shared by every device call.
 hswa_status check_shape(const hswa_shape *sh) {
   if (!sh) return HSWA_ERR_INVALID_ARG;
@@ -506,6 +511,7 @@ size_t hswa_decode_shared_workspace_bytes(const hswa_shape *shape, int32_t ns, i
   if (num_queries < 1 || num_queries > kMaxQueries || max_shared_len < 0) return 0;
   if (!shared_fits(shape, ns, num_groups, max_context_len, max_shared_len))
     return hswa_decode_multi_workspace_bytes(shape, ns, num_queries, max_context_len);
+  if (too_many_rows(shape, ns, num_queries)) return 0;
   return shared_geometry(shape, ns, max_context_len, num_queries, num_groups).total_bytes;
 }
 
@@ -526,7 +532,7 @@ hswa_status hswa_decode_shared(hswa_layer layer, const hswa_shape *shape, const 
   if ((st = make_pool(layer, shape, cache, p.d.pool)) != HSWA_OK) return st;
   if ((int64_t)cache->table_stride * shape->page_size < (int64_t)max_context_len) return HSWA_ERR_CAPACITY;
   if (!q || !context_lens || !out || !workspace) return HSWA_ERR_INVALID_ARG;
-  if ((int64_t)ns * num_queries * shape->num_q_heads > kMaxRows) return HSWA_ERR_UNSUPPORTED;
+  if (too_many_rows(shape, ns, num_queries)) return HSWA_ERR_UNSUPPORTED;
   const SharedGeometry geo = shared_geometry(shape, ns, max_context_len, num_queries, num_groups);
   if (workspace_bytes < geo.total_bytes) return HSWA_ERR_CAPACITY;
   decode_params(p.d, shape, q, context_lens, ns, num_queries, max_context_len, out);
@@ -542,6 +548,7 @@ size_t hswa_decode_scored_workspace_bytes(const hswa_shape *shape, int32_t ns, i
                                           int32_t max_context_len) {
   if (check_shape(shape) != HSWA_OK || ns < 1 || max_context_len < 1) return 0;
   if (num_queries < 1 || num_queries > kMaxQueries || max_context_len > kMaxLen) return 0;
+  if (too_many_rows(shape, ns, num_queries)) return 0;
   return scored_geometry(shape, ns, max_context_len, num_queries).total_bytes;
 }
 
@@ -561,7 +568,7 @@ hswa_status hswa_decode_scored(hswa_layer layer, const hswa_shape *shape, const 
   if (score_stride < max_context_len) return HSWA_ERR_CAPACITY;
   if (ns == 0) return HSWA_OK;
   if (!q || !context_lens || !out || !scores_out || !workspace) return HSWA_ERR_INVALID_ARG;
-  if ((int64_t)ns * num_queries * shape->num_q_heads > kMaxRows) return HSWA_ERR_UNSUPPORTED;
+  if (too_many_rows(shape, ns, num_queries)) return HSWA_ERR_UNSUPPORTED;
   const ScoredGeometry geo = scored_geometry(shape, ns, max_context_len, num_queries);
   if (workspace_bytes < geo.total_bytes) return HSWA_ERR_CAPACITY;
   decode_params(p.s.d, shape, q, context_lens, ns, num_queries, max_context_len, out);
