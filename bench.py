@@ -55,14 +55,14 @@ FLUSH_BYTES = 1 << 30  # a write this large evicts the 256 MB memory-side cache
 # measured again.
 MEASURED_TRAFFIC = {
     "decode_full_stack70": {"sources": ["decode_kernels.h", "decode.hip", "hswa_common.h", "hswa_launch.h"],
-                            "sha256": "db90c0e4d02000fca79586e644b544144f0c6ce35d5c618a508afdb7993d1f0f",
-                            "fetch_bytes": 8609234479, "write_bytes": 5574350},
+                            "sha256": "53ea6538a6c0e66e7eb85904a28717c1e1d7ba1590cb8c831684596a2bd57302",
+                            "fetch_bytes": 8609236492, "write_bytes": 5574564},
     "prefill_full": {"sources": ["prefill.hip", "hswa_common.h", "hswa_launch.h"],
-                     "sha256": "361c9927c2011310a59e80866afa7d153ff85834f6570c094696ea09f44561fc",
-                     "fetch_bytes": 452863023, "write_bytes": 141388810},
+                     "sha256": "f1bce45d9df9e130bf2e3ce275c6e0fdfc26aab850725f78450c7608b8bc69cc",
+                     "fetch_bytes": 452861522, "write_bytes": 141337261},
     "prefill_swa": {"sources": ["prefill_run.hip", "hswa_common.h", "hswa_launch.h"],
-                    "sha256": "0fc0198dc3887a979c26c093b9e4c18919f475136d76e63f15ec6049d97bdbe6",
-                    "fetch_bytes": 184857995, "write_bytes": 147068669},
+                    "sha256": "720c93642dbd146f37e04c1fb15bfe400fb6aff0db47c1f1ab419de4894f0e3b",
+                    "fetch_bytes": 184857383, "write_bytes": 148127928},
 }
 
 

@@ -342,7 +342,9 @@ hswa_status hswa_decode_multi(hswa_layer layer, const hswa_shape *shape, const h
  * count), read through the row of the group's first sequence with a context;
  * the rest, and sequences of no group, are read as hswa_decode_multi reads them.
  * Every row of the table is complete all the same: which entries are read is no
- * part of the contract. The outputs are hswa_decode_multi's up to rounding.
+ * part of the contract. The outputs are hswa_decode_multi's up to rounding (both
+ * round the probabilities to bf16 for their product with V; maxima, sums and
+ * partial rows are fp32).
  * cu_groups: device int32 [num_groups + 1], non-decreasing, within [0, ns];
  * shared_lens: device int32 [num_groups] (values above max_shared_len are
  * clamped to it, values below 64 share nothing); num_groups <= ns;
@@ -379,7 +381,10 @@ hswa_status hswa_decode_shared(hswa_layer layer, const hswa_shape *shape, const 
  * a page id outside the pool is left out, as in hswa_decode, and adds nothing.
  * The other arguments and the output rows are as in hswa_decode_multi (rows may
  * differ from its in the last bit: their sums are not of rounded probabilities);
- * workspace >= hswa_decode_scored_workspace_bytes, for contexts of any length.
+ * workspace >= hswa_decode_scored_workspace_bytes, for contexts of any length: up
+ * to num_queries * Hq / Hkv = 16 it holds every score of the call, 4 * ns *
+ * num_queries * Hq * max_context_len bytes (16 sequences, 64 heads, 65536: 0.27
+ * GB), so a close bound saves memory.
  * HSWA_ERR_UNSUPPORTED: an SWA layer (it evicts by its window), more than 2^25
  * rows (ns * num_queries * Hq), a max_context_len over 2^30 (a size of 0). */
 size_t hswa_decode_scored_workspace_bytes(const hswa_shape *shape, int32_t ns, int32_t num_queries,

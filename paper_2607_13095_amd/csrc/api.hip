@@ -222,6 +222,8 @@ ScoredGeometry scored_geometry(const hswa_shape *sh, int32_t ns, int32_t max_ctx
 //                  32 x 4000               63      24 / 20
 //   16 / 16        2 x 4000, 2 x 8000      33, 66  21 / 22, 24 / 31
 //                  32 x 256                65      25 / 28
+// (63 - 66 MB go both ways, so the limit stands above them: up to 9 us are given up
+// there, rather than 4 lost.)
 bool shared_fits(const hswa_shape *sh, int32_t ns, int32_t num_groups, int32_t max_context_len,
                  int32_t max_shared_len) {
   constexpr double kLeastSaved = 70e6;

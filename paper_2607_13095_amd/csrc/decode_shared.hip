@@ -660,7 +660,9 @@ __device__ __forceinline__ void prefix_tiles(const SharedParams &p, TileBufs &bu
   // tile's exponentials taken again, only if some lane's share of a row sum
   // exceeds 2^12 (an infinite one counts): numerator and denominator share the
   // maximum, so the result is the same. It starts at -FLT_MAX, so that a masked
-  // score gives 0 and the first finite one raises it.
+  // score gives 0 and the first finite one raises it. The probabilities go to the
+  // PV product in bf16, as those of the own keys do (decode_kernels.h: why, and what
+  // it costs); sums, maxima and partial rows are fp32.
   auto tile_exp = [&](const f32x4 (&sc)[2][2][kCG], u32x4 (&pf)[2][kCG], float (&ts)[kCG]) {
 #pragma unroll
     for (int cg = 0; cg < kCG; ++cg) {

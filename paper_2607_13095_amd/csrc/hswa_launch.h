@@ -149,11 +149,14 @@ struct SharedParams {
 };
 
 // Decode that also adds every key's attention weight to a score (decode_scored.hip).
-// Up to this many (query, head) columns of a KV head the scores are stored, 4
-// bytes for each of a key's columns. 64 / 8 heads, 16 sequences, us a call with
-// them stored and formed anew: 24 columns (3 queries) over 2 - 16K keys 186 and
-// 213, over 30 - 32K 558 and 567; 32 columns 205 and 216, 620 and 570. From there
-// on it is the workspace that counts: 32 columns of 16 x 64K keys take 1.1 GB.
+// Up to this many (query, head) columns of a KV head, one column group of a wave,
+// the scores are stored: 4 bytes for each column of a key, for max_ctx keys of every
+// sequence whatever its length. 64 / 8 heads, 16 sequences, us a call with them
+// stored (by two column groups a wave) and formed anew: 24 columns (3 queries) over
+// 2 - 16K keys 186 and 213, over 30 - 32K 558 and 567; 32 columns 205 and 216, 620
+// and 570. So 17 - 24 columns would gain 2 - 13% by storing, and 32 lose 9% on long
+// contexts; both are formed anew for the workspace's sake, which takes 0.54 GB for
+// 16 columns of 16 x 64K keys already, and would take 0.8 and 1.1.
 constexpr int kKeepColumns = 16;
 struct ScoredParams {
   SharedParams s;          // s.d: split, with ws_s; or with row_lse, all of s, each sequence a group
