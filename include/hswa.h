@@ -354,8 +354,8 @@ hswa_status hswa_decode_multi(hswa_layer layer, const hswa_shape *shape, const h
  * bit for bit, where reading the prefixes once cannot gain: an SWA layer (it reads
  * its window), no group, one sequence, prefixes below 64, and calls whose
  * (ns - num_groups) * max_shared_len positions hold less than 70 MB, or whose
- * max_context_len is over 2^30. HSWA_ERR_UNSUPPORTED beside hswa_decode_multi's:
- * over 2^25 rows (ns * num_queries * Hq) in any other call (a size of 0).
+ * max_context_len is at most 256 or over 2^30. HSWA_ERR_UNSUPPORTED beside
+ * hswa_decode_multi's: over 2^25 rows (ns * num_queries * Hq) in any other call (a size of 0).
  * The other arguments are as in hswa_decode_multi. */
 size_t hswa_decode_shared_workspace_bytes(const hswa_shape *shape, int32_t ns, int32_t num_queries,
                                           int32_t max_context_len, int32_t num_groups, int32_t max_shared_len);

@@ -224,10 +224,18 @@ ScoredGeometry scored_geometry(const hswa_shape *sh, int32_t ns, int32_t max_ctx
 //                  32 x 256                65      25 / 28
 // (63 - 66 MB go both ways, so the limit stands above them: up to 9 us are given up
 // there, rather than 4 lost.)
+// Contexts of up to 256 keys, the shortest span, hswa_decode_multi takes in one pass
+// and one launch, the shared pages out of the caches: of 113 such batches (8 - 400
+// sequences, 64 - 250 shared keys, 1 - 8 queries) that save 70 MB and more, each took
+// 1.06 to 6.4 times as long by prefix (64 / 8 heads, 84 sequences, 2 queries 51 / 9;
+// 32 / 32, 336, 8 queries 443 / 89). Longer contexts over fewer than 256 shared keys
+// go both ways (0.6 - 1.8), over 384 and more mostly one (0.27 - 1.43, 0.74 in the mean).
 bool shared_fits(const hswa_shape *sh, int32_t ns, int32_t num_groups, int32_t max_context_len,
                  int32_t max_shared_len) {
   constexpr double kLeastSaved = 70e6;
-  if (ns < 2 || num_groups < 1 || max_shared_len < hswa::kSharedTile || max_context_len > kMaxLen) return false;
+  constexpr int32_t kOnePass = 256;
+  if (ns < 2 || num_groups < 1 || max_shared_len < hswa::kSharedTile) return false;
+  if (max_context_len <= kOnePass || max_context_len > kMaxLen) return false;
   const double keys = (double)(ns - num_groups) * (max_shared_len < max_context_len ? max_shared_len : max_context_len);
   return keys * sh->num_kv_heads * (sh->head_dim * 4) >= kLeastSaved;
 }

@@ -12,6 +12,7 @@ from oracle import eviction as OE
 from paper_2607_13095_amd import hswa
 from paper_2607_13095_amd.kvcache import prefix_groups
 from tests.hswa_testlib import assert_close, i32, to_dev, to_f64
+from tests.test_gpu_decode_shared import Shared
 from tests.test_gpu_kv_evict import Evict, _scores
 
 pytestmark = pytest.mark.gpu
@@ -92,6 +93,24 @@ def test_every_round_of_two_at_once(gpu_lib):
                 c.compare(want)
     torch.cuda.synchronize()
     assert not bool(both[0].bad) and not bool(both[1].bad)
+
+
+@pytest.mark.parametrize("max_ctx", [256, 257])
+@pytest.mark.parametrize("nq", [1, 3])
+def test_shared_decode_about_one_pass(gpu_lib, max_ctx, nq):
+    """Contexts of up to 256 keys are hswa_decode_multi's, bit for bit and without a
+    workspace; one key more is shared."""
+    r = np.random.default_rng(max_ctx + nq)
+    s = Shared([(190, [int(x) for x in r.integers(nq, 67, 90)]), (64, [int(x) for x in r.integers(nq, 100, 70)])], nq, 16,
+               8, 64, (1713, nq), max_ctx=max_ctx)
+    got = s.run(max_shared=190)
+    assert (s.ws.numel() > 1) == (max_ctx > 256)
+    s.check(got, f"contexts of {max_ctx}", by_prefix=max_ctx > 256)
+    if max_ctx == 256:
+        out = torch.full_like(s.q, 7.0)
+        hswa.decode_multi(*s.args[:6], out)
+        torch.cuda.synchronize()
+        assert np.array_equal(to_f64(out), got)
 
 
 @pytest.mark.parametrize("max_ctx,max_keep", [(500, 96), (500, 600), (9000, 3000), (33000, 96)])
